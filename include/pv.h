@@ -334,6 +334,115 @@ pv_status pv_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *q_out
                                     int32_t max_pos, int32_t style, const int32_t *page_table,
                                     void *k_pages, void *v_pages, void *stream);
 
+/*
+ * Norms of queries and keys for each head, in the same pass as the rotation and the append: for models
+ * that normalise q and k in front of the rotary embedding.  Each row x of D elements (one token, one
+ * head) becomes
+ *     y = x * w / sqrt(mean(x^2) + eps)
+ * and is then rotated and stored as by pv_rope_kv_append_planned; V is moved as there.  fp32
+ * throughout (the sum of squares too), rounded to the 16-bit type once, behind the rotation.
+ *   q_weight, k_weight : device [D] of the pool's type, 16-byte aligned, shared by all heads; NULL =
+ *                        rows of that kind are not normalised, only rotated
+ *   eps                : finite and positive, else PV_ERR_INVALID_ARG (a row of zeros stays zero)
+ * Everything else as for pv_rope_kv_append_planned.  One launch, asynchronous, no allocation.
+ */
+pv_status pv_norm_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *q_out,
+                                         const void *k_new, const void *v_new,
+                                         const void *q_weight, const void *k_weight, float eps,
+                                         const float *cos_sin, int32_t max_pos, int32_t style,
+                                         const int32_t *page_table, void *k_pages, void *v_pages,
+                                         void *stream);
+
+/*
+ * 8-bit pools: K and V as codes of 8 bits with a scale for each block, half the memory and half the
+ * bytes that attention reads.  A block is one page (16 tokens) of one KV head, K and V apart.
+ *
+ * A code is an e4m3 value: sign, 4 bits of exponent (bias 7), 3 of mantissa, no infinity, NaN = 0x7F
+ * (0xFF), largest 448, smallest 2^-9.  A scale is a power of two 2^e, held as the byte e + 127; code and
+ * scale stand for code * 2^e.  e lies in -15 .. 8 for f16 and -117 .. 120 for bf16, so that this is
+ * always a value of the pool description's 16-bit type.  Layout (bytes; P = 16, one pool for K and
+ * one for V, pv_kv8_pool_bytes each; scales [num_pages][Hkv], pv_kv8_scale_bytes each):
+ *   K(page p, head h, slot s, dim d) at (p*Hkv+h)*P*D + (s/4)*4*D + (d/16)*64 + (s%4)*16 + d%16
+ *   V(page p, head h, slot s, dim d) at (p*Hkv+h)*P*D + d*16 + s
+ *   scale of (page p, head h)        at p*Hkv + h
+ * Codes and scales of pages that hold no tokens may be anything; codes of slots past the end of a
+ * request's last page too.
+ *
+ * The pv_pool_desc is that of the rows: dtype is the 16-bit type of q, out, k_new and v_new.  The calls
+ * take plans made by pv_plan_create_kv8 and refuse others (PV_ERR_INVALID_ARG), as the calls for 16-bit
+ * pools refuse these.  The plan's accessors, upload, timing and pv_plan_check_page_table work as for
+ * other plans; with check_append_unique the latter demands that a page that receives new tokens appears
+ * in no other request with new tokens in that page (one page has one scale, which one writer sets).
+ */
+typedef struct {
+    void *k, *v;                  /* device, 16-byte aligned */
+    uint8_t *k_scales, *v_scales; /* device */
+} pv_kv8_pool;
+
+size_t pv_kv8_pool_bytes(const pv_pool_desc *pool);  /* of ONE pool (K or V); 0 if invalid */
+size_t pv_kv8_scale_bytes(const pv_pool_desc *pool); /* of the scales of ONE pool; 0 if invalid */
+/* Byte offsets inside a pool (host helpers); -1 on an invalid description or index. */
+int64_t pv_kv8_k_offset(const pv_pool_desc *pool, int32_t page, int32_t head, int32_t slot,
+                        int32_t d);
+int64_t pv_kv8_v_offset(const pv_pool_desc *pool, int32_t page, int32_t head, int32_t slot,
+                        int32_t d);
+
+/* As pv_plan_create, for 8-bit pools.  pv_plan_is_kv8: 1, 0, or -1 for NULL. */
+pv_status pv_plan_create_kv8(const pv_pool_desc *pool, int32_t num_q_heads,
+                             const int32_t *ctx_lens /* host [num_reqs] */,
+                             const int32_t *q_lens /* host [num_reqs] */, int32_t num_reqs,
+                             int32_t max_pages_per_req, pv_plan **plan);
+int32_t pv_plan_is_kv8(const pv_plan *plan);
+
+/*
+ * KV append into 8-bit pools: the rows go to the positions that pv_kv_append_planned gives them.  For
+ * the new rows of a block let a be the largest finite magnitude among them (0 if there is none) and n
+ * the least exponent of the range above with a <= 448 * 2^n.  If the block's first new token lies in
+ * slot 0 the page is begun: e = n, whatever it held.  Otherwise e = max(n, the block's e), and where
+ * that is more than it was, the codes of the slots in front of the first new token become
+ * round(code * 2^(old e - e)).  New codes are round(x / 2^e); with the largest e, finite values are
+ * limited to 240 * 2^e first (256 * 2^e is past the 16-bit type).  Infinities and NaN become NaN.
+ * round: to the nearest code, ties to even.  The result is unique, bit for bit.  Codes of other
+ * slots, those behind the new tokens among them, keep their bits (not their meaning, if the
+ * scale changes).
+ *   k_new, v_new : device [total_q, Hkv, D], 16-byte aligned
+ * One launch, asynchronous, no allocation.
+ */
+pv_status pv_kv8_append_planned(pv_plan *plan, const void *k_new, const void *v_new,
+                                const int32_t *page_table, const pv_kv8_pool *pool, void *stream);
+
+/* pv_norm_rope_kv_append_planned into 8-bit pools: queries and keys are rotated (and normalised, where
+ * a weight is given) and rounded to 16 bits as there, and keys and values then go through
+ * pv_kv8_append_planned, in one launch. */
+pv_status pv_kv8_norm_rope_append_planned(pv_plan *plan, const void *q_in, void *q_out,
+                                          const void *k_new, const void *v_new,
+                                          const void *q_weight, const void *k_weight, float eps,
+                                          const float *cos_sin, int32_t max_pos, int32_t style,
+                                          const int32_t *page_table, const pv_kv8_pool *pool,
+                                          void *stream);
+
+/*
+ * The inverse of the append: the rows at the positions of the plan's new tokens, ctx_lens[r] ..
+ * ctx_lens[r] + q_lens[r] - 1 of every request, as code * 2^e in the 16-bit type (exact).  To read
+ * whole histories back, make a plan with ctx_lens 0.
+ *   k_rows, v_rows : device [total_q, Hkv, D], 16-byte aligned
+ * One launch, asynchronous, no allocation.
+ */
+pv_status pv_kv8_read_planned(pv_plan *plan, const pv_kv8_pool *pool, const int32_t *page_table,
+                              void *k_rows, void *v_rows, void *stream);
+
+/*
+ * Multi-token paged attention over 8-bit pools: pv_multi_token_paged_attn_planned with K, V = code *
+ * 2^e.  Codes are widened to the 16-bit type on the way to the matrix cores, which is exact; everything
+ * behind that is as there (scores, softmax and sums in fp32, probabilities and results rounded to
+ * 16 bits).  Arguments, workspace and launches as there.
+ */
+pv_status pv_kv8_multi_token_paged_attn_planned(pv_plan *plan, const void *q,
+                                                const pv_kv8_pool *pool,
+                                                const int32_t *page_table, float scale, void *out,
+                                                void *workspace, size_t workspace_bytes,
+                                                void *stream);
+
 /* Host: table[t*D + i] = cos(t * base^(-2i/D)), table[t*D + D/2 + i] = sin(same), t < max_pos,
  * i < D/2, evaluated in double precision and rounded to float.  PV_ERR_INVALID_ARG unless
  * base > 0, head_dim is even and positive, max_pos >= 0 and table is not NULL. */

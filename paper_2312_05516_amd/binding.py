@@ -39,6 +39,10 @@ EXPORTS = [
     "pv_pages_gather", "pv_pages_scatter", "pv_cost_model", "pv_retention_order",
     "pv_rope_kv_append_planned", "pv_rope_table",
     "pv_multi_token_paged_attn_noalloc", "pv_static_scratch_bytes",
+    "pv_norm_rope_kv_append_planned", "pv_kv8_pool_bytes", "pv_kv8_scale_bytes",
+    "pv_kv8_k_offset", "pv_kv8_v_offset", "pv_plan_create_kv8", "pv_plan_is_kv8",
+    "pv_kv8_append_planned", "pv_kv8_norm_rope_append_planned", "pv_kv8_read_planned",
+    "pv_kv8_multi_token_paged_attn_planned",
 ]
 
 
@@ -52,6 +56,10 @@ class PoolDesc(ctypes.Structure):
     _fields_ = [("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("dtype", ctypes.c_int32)]
+
+
+class _Kv8Ptrs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales")]
 
 
 if not os.path.exists(LIB_PATH):
@@ -136,6 +144,30 @@ _lib.pv_rope_table.argtypes = [ctypes.c_double, ctypes.c_int32, ctypes.c_int32,
                                ctypes.POINTER(ctypes.c_float)]
 _lib.pv_attn_workspace_bytes.restype = ctypes.c_size_t
 _lib.pv_attn_workspace_bytes.argtypes = [_descp] + [ctypes.c_int32] * 4
+_lib.pv_norm_rope_kv_append_planned.restype = ctypes.c_int
+_lib.pv_norm_rope_kv_append_planned.argtypes = (
+    [_vp] * 7 + [ctypes.c_float, _vp, ctypes.c_int32, ctypes.c_int32] + [_vp] * 4)
+for _n in ("pv_kv8_pool_bytes", "pv_kv8_scale_bytes"):
+    getattr(_lib, _n).restype = ctypes.c_size_t
+    getattr(_lib, _n).argtypes = [_descp]
+for _n in ("pv_kv8_k_offset", "pv_kv8_v_offset"):
+    getattr(_lib, _n).restype = ctypes.c_int64
+    getattr(_lib, _n).argtypes = [_descp] + [ctypes.c_int32] * 4
+_lib.pv_plan_create_kv8.restype = ctypes.c_int
+_lib.pv_plan_create_kv8.argtypes = _lib.pv_plan_create.argtypes
+_lib.pv_plan_is_kv8.restype = ctypes.c_int32
+_lib.pv_plan_is_kv8.argtypes = [_vp]
+_kv8p = ctypes.POINTER(_Kv8Ptrs)
+_lib.pv_kv8_append_planned.restype = ctypes.c_int
+_lib.pv_kv8_append_planned.argtypes = [_vp] * 4 + [_kv8p, _vp]
+_lib.pv_kv8_norm_rope_append_planned.restype = ctypes.c_int
+_lib.pv_kv8_norm_rope_append_planned.argtypes = (
+    [_vp] * 7 + [ctypes.c_float, _vp, ctypes.c_int32, ctypes.c_int32, _vp, _kv8p, _vp])
+_lib.pv_kv8_read_planned.restype = ctypes.c_int
+_lib.pv_kv8_read_planned.argtypes = [_vp, _kv8p] + [_vp] * 4
+_lib.pv_kv8_multi_token_paged_attn_planned.restype = ctypes.c_int
+_lib.pv_kv8_multi_token_paged_attn_planned.argtypes = [_vp, _vp, _kv8p, _vp, ctypes.c_float, _vp, _vp,
+                                                       ctypes.c_size_t, _vp]
 
 
 # ------------------------------------------------------------------ marshalling helpers
@@ -235,15 +267,30 @@ class Plan:
             pass
 
 
-def plan_create(desc: PoolDesc, num_q_heads: int, ctx_lens, q_lens,
-                max_pages_per_req: int) -> Plan:
+def _plan_create(where: str, desc: PoolDesc, num_q_heads: int, ctx_lens, q_lens,
+                 max_pages_per_req: int) -> Plan:
     cl, ql = _host_i32(ctx_lens), _host_i32(q_lens)
     if cl.shape != ql.shape or cl.ndim != 1:
         raise ValueError("ctx_lens and q_lens must be 1-D and of equal length")
     h = _vp()
-    _check(_lib.pv_plan_create(ctypes.byref(desc), int(num_q_heads), _i32(cl), _i32(ql), len(cl),
-                               int(max_pages_per_req), ctypes.byref(h)), "pv_plan_create")
+    _check(getattr(_lib, where)(ctypes.byref(desc), int(num_q_heads), _i32(cl), _i32(ql), len(cl),
+                                int(max_pages_per_req), ctypes.byref(h)), where)
     return Plan(h.value, desc, int(num_q_heads), len(cl))
+
+
+def plan_create(desc: PoolDesc, num_q_heads: int, ctx_lens, q_lens,
+                max_pages_per_req: int) -> Plan:
+    return _plan_create("pv_plan_create", desc, num_q_heads, ctx_lens, q_lens, max_pages_per_req)
+
+
+def plan_create_kv8(desc: PoolDesc, num_q_heads: int, ctx_lens, q_lens,
+                    max_pages_per_req: int) -> Plan:
+    return _plan_create("pv_plan_create_kv8", desc, num_q_heads, ctx_lens, q_lens,
+                        max_pages_per_req)
+
+
+def plan_is_kv8(plan: Plan) -> bool:
+    return bool(_lib.pv_plan_is_kv8(plan.handle))
 
 
 def plan_destroy(plan: Plan):
@@ -343,6 +390,71 @@ def rope_kv_append_planned(plan: Plan, q_in, q_out, k_new, v_new, cos_sin, style
                                           _ptr(v_new), _ptr(cos_sin), int(cos_sin.shape[0]), st,
                                           _ptr(page_table), _ptr(k_pages), _ptr(v_pages),
                                           _stream(stream)), "pv_rope_kv_append_planned")
+
+
+def norm_rope_kv_append_planned(plan: Plan, q_in, q_out, k_new, v_new, q_weight, k_weight, eps,
+                                cos_sin, style, page_table, k_pages, v_pages, stream=None):
+    """As rope_kv_append_planned, queries and keys normalised first where a weight [D] is given."""
+    st = ROPE_STYLES[style] if isinstance(style, str) else int(style)
+    _check(_lib.pv_norm_rope_kv_append_planned(
+        plan.handle, _ptr(q_in), _ptr(q_out), _ptr(k_new), _ptr(v_new), _ptr(q_weight),
+        _ptr(k_weight), float(eps), _ptr(cos_sin), int(cos_sin.shape[0]), st, _ptr(page_table),
+        _ptr(k_pages), _ptr(v_pages), _stream(stream)), "pv_norm_rope_kv_append_planned")
+
+
+class Kv8Pool:
+    """The four device arrays of an 8-bit K/V pool (kept alive): codes of K and V, of
+    kv8_pool_bytes(desc) bytes each, and their scales, of kv8_scale_bytes(desc) bytes each."""
+
+    def __init__(self, k, v, k_scales, v_scales):
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self._ptrs = _Kv8Ptrs(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales))
+
+
+def kv8_pool_bytes(desc: PoolDesc) -> int:
+    return int(_lib.pv_kv8_pool_bytes(ctypes.byref(desc)))
+
+
+def kv8_scale_bytes(desc: PoolDesc) -> int:
+    return int(_lib.pv_kv8_scale_bytes(ctypes.byref(desc)))
+
+
+def kv8_k_offset(desc: PoolDesc, page: int, head: int, slot: int, d: int) -> int:
+    return int(_lib.pv_kv8_k_offset(ctypes.byref(desc), page, head, slot, d))
+
+
+def kv8_v_offset(desc: PoolDesc, page: int, head: int, slot: int, d: int) -> int:
+    return int(_lib.pv_kv8_v_offset(ctypes.byref(desc), page, head, slot, d))
+
+
+def kv8_append_planned(plan: Plan, k_new, v_new, page_table, pool: Kv8Pool, stream=None):
+    _check(_lib.pv_kv8_append_planned(plan.handle, _ptr(k_new), _ptr(v_new), _ptr(page_table),
+                                      ctypes.byref(pool._ptrs), _stream(stream)),
+           "pv_kv8_append_planned")
+
+
+def kv8_norm_rope_append_planned(plan: Plan, q_in, q_out, k_new, v_new, q_weight, k_weight, eps,
+                                 cos_sin, style, page_table, pool: Kv8Pool, stream=None):
+    """As norm_rope_kv_append_planned, into 8-bit pools."""
+    st = ROPE_STYLES[style] if isinstance(style, str) else int(style)
+    _check(_lib.pv_kv8_norm_rope_append_planned(
+        plan.handle, _ptr(q_in), _ptr(q_out), _ptr(k_new), _ptr(v_new), _ptr(q_weight),
+        _ptr(k_weight), float(eps), _ptr(cos_sin), int(cos_sin.shape[0]), st, _ptr(page_table),
+        ctypes.byref(pool._ptrs), _stream(stream)), "pv_kv8_norm_rope_append_planned")
+
+
+def kv8_read_planned(plan: Plan, pool: Kv8Pool, page_table, k_rows, v_rows, stream=None):
+    _check(_lib.pv_kv8_read_planned(plan.handle, ctypes.byref(pool._ptrs), _ptr(page_table),
+                                    _ptr(k_rows), _ptr(v_rows), _stream(stream)),
+           "pv_kv8_read_planned")
+
+
+def kv8_multi_token_paged_attn_planned(plan: Plan, q, pool: Kv8Pool, page_table, scale: float, out,
+                                       workspace=None, stream=None):
+    _check(_lib.pv_kv8_multi_token_paged_attn_planned(
+        plan.handle, _ptr(q), ctypes.byref(pool._ptrs), _ptr(page_table), float(scale), _ptr(out),
+        _ptr(workspace), _nbytes(workspace), _stream(stream)),
+        "pv_kv8_multi_token_paged_attn_planned")
 
 
 def multi_token_paged_attn_planned(plan: Plan, q, k_pages, v_pages, page_table, scale: float, out,

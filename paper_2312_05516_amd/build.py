@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libpv.so")
 OBJ = os.path.join(HERE, "_build")
 
 SOURCES = ["pv_plan.cpp", "pv_lib.hip", "pv_append.hip", "pv_attn_narrow.hip", "pv_attn_wide.hip", "pv_attn_tile256.hip",
-           "pv_swap.hip", "pv_rope.hip"]
+           "pv_swap.hip", "pv_rope.hip", "pv_kv8.hip", "pv_attn_kv8_narrow.hip"]
 # packed fp32 VALU forms are switched off for every device compile
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

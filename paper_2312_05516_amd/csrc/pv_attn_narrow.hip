@@ -16,7 +16,7 @@
 // query row: the softmax needs no cross-lane traffic beyond two exchanges for the running
 // maximum, and the probabilities are already laid out as the B operand of O^T += V^T P^T.  The
 // four partial (max, sum, O) triples are merged through LDS at the end.
-#include "pv_device.h"
+#include "pv_narrow.h"
 
 namespace pv {
 
@@ -239,70 +239,8 @@ __global__ __launch_bounds__(256, 2) void attn_narrow_kernel(
 
     if constexpr (AHEAD) asm volatile("" ::"v"(touched));
 
-    // ---- merge the four wavefronts ----
-    float l_tot = l_run + __shfl_xor(l_run, 16);
-    l_tot += __shfl_xor(l_tot, 32);
-    if (g == 0) {
-        sm_m[w][q16] = m_run;
-        sm_l[w][q16] = l_tot;
-    }
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk)
-        *reinterpret_cast<f32x4 *>(&sm_o[w][q16][16 * blk + 4 * g]) = o[blk];
-    __syncthreads();
-
-    constexpr int PER = D / 16;  // output elements per thread
-    const int r16 = (int)threadIdx.x >> 4;
-    const int d0 = ((int)threadIdx.x & 15) * PER;
-    if (r16 >= it.row_count) return;
-    float mw[NW], wgt[NW];
-    float M = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        mw[i] = sm_m[i][r16];
-        M = fmaxf(M, mw[i]);
-    }
-    const float M_safe = M == -INFINITY ? 0.f : M;
-    float L = 0.f;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        wgt[i] = fast_exp2(mw[i] - M_safe);
-        L += wgt[i] * sm_l[i][r16];
-    }
-    float acc[PER];
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        float a = 0.f;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) a += wgt[i] * sm_o[i][r16][d0 + e];
-        acc[e] = a;
-    }
-    const int orow = it.row_begin + r16;
-    if (it.split_count == 1) {
-        const float inv = 1.f / L;
-        const int otok = orow / group;
-        const int ohq = it.kv_head * group + orow % group;
-        uint16_t *dst = out + ((int64_t)(it.q_row0 + otok) * num_q_heads + ohq) * D + d0;
-        uint32_t packed[PER / 2];
-#pragma unroll
-        for (int e = 0; e < PER / 2; ++e)
-            packed[e] = T::pack2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-        if constexpr (PER == 8) {
-            *reinterpret_cast<u32x4 *>(dst) = u32x4{packed[0], packed[1], packed[2], packed[3]};
-        } else {
-            *reinterpret_cast<u32x2 *>(dst) = u32x2{packed[0], packed[1]};
-        }
-    } else {
-        const int64_t slot = (int64_t)it.partial_base + r16;
-        float *po = ws_o + slot * D + d0;
-#pragma unroll
-        for (int e = 0; e < PER; e += 4)
-            *reinterpret_cast<f32x4 *>(po + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-        if (((int)threadIdx.x & 15) == 0) {
-            ws_ml[2 * slot] = M;
-            ws_ml[2 * slot + 1] = L;
-        }
-    }
+    finish_narrow_item<T, D>(it, group, num_q_heads, o, m_run, l_run, sm_o, sm_m, sm_l, out, ws_o,
+                             ws_ml);
 }
 
 // Merge of split-KV partial results: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s. One

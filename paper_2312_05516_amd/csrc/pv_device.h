@@ -149,6 +149,48 @@ __device__ __forceinline__ typename T::vec8 as_vec8(u32x4 raw)
     return __builtin_bit_cast(typename T::vec8, raw);
 }
 
+template <typename T>
+__device__ __forceinline__ void unpack8(u32x4 raw, float (&x)[8])
+{
+    const typename T::vec8 v = as_vec8<T>(raw);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+}
+
+template <typename T>
+__device__ __forceinline__ u32x4 pack8(const float (&x)[8])
+{
+    return u32x4{T::pack2(x[0], x[1]), T::pack2(x[2], x[3]), T::pack2(x[4], x[5]),
+                 T::pack2(x[6], x[7])};
+}
+
+// The pair (a, b) turned by the angle of cosine c and sine s, with the roundings spelled out, so that
+// every kernel that uses it gets the same bits in front of the rounding to 16 bits.
+__device__ __forceinline__ void rotate_pair(float a, float b, float c, float s, float &x, float &y)
+{
+    x = __builtin_fmaf(a, c, -(b * s));
+    y = __builtin_fmaf(a, s, b * c);
+}
+
+// Norm of a row of D elements: 1 / sqrt(mean of the squares + eps).  The squares of 8 elements are
+// added in order, those of chunk i (of 8) and of chunk i + D/16, then neighbours: `pairs` holds such
+// a sum of two chunks for each of the D/16 lanes of a row, or of PER consecutive ones for fewer lanes.
+// So every kernel that normalises rows gets the same bits, however it spreads a row over lanes.
+__device__ __forceinline__ float sum_squares(const float (&x)[8])
+{
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += x[e] * x[e];
+    return s;
+}
+template <int D, int PER = 1>
+__device__ __forceinline__ float norm_factor(float pairs, float eps)
+{
+#pragma unroll
+    for (int m = 1; m < D / 16 / PER; m *= 2) pairs += __shfl_xor(pairs, m);
+    return 1.f / sqrtf(pairs * (1.f / D) + eps);
+}
+
 // whether one of eight 16-bit values is an infinity or a NaN
 template <typename T>
 __device__ __forceinline__ bool any_not_finite(u32x4 raw)

@@ -32,10 +32,18 @@ hipError_t launch_attn_tile256(const pv_plan *plan, const DeviceLists &dl, const
 hipError_t launch_attn_combine(const pv_plan *plan, const DeviceLists &dl, const float *ws_o,
                                const float *ws_ml, void *out, hipStream_t stream);
 
-hipError_t launch_rope_append(const pv_plan *plan, const DeviceLists &dl, int style,
-                              const void *q_in, void *q_out, const void *k_new,
-                              const void *v_new, const float *cos_sin, const int32_t *page_table,
+hipError_t launch_rope_append(const pv_plan *plan, const DeviceLists &dl, const NormRope &nr,
+                              const void *k_new, const void *v_new, const int32_t *page_table,
                               void *k_pages, void *v_pages, hipStream_t stream);
+hipError_t launch_kv8_append(const pv_plan *plan, const DeviceLists &dl, const NormRope &nr,
+                             const void *k_new, const void *v_new, const int32_t *page_table,
+                             const pv_kv8_pool &pool, hipStream_t stream);
+hipError_t launch_kv8_read(const pv_plan *plan, const DeviceLists &dl, const pv_kv8_pool &pool,
+                           const int32_t *page_table, void *k_rows, void *v_rows,
+                           hipStream_t stream);
+hipError_t launch_attn_kv8_narrow(const pv_plan *plan, const DeviceLists &dl, const void *q,
+                                  const pv_kv8_pool &pool, const int32_t *page_table, float scale,
+                                  void *out, float *ws_o, float *ws_ml, hipStream_t stream);
 hipError_t launch_pages_copy(bool gather, const pv_pool_desc *pool, const int32_t *page_ids,
                              int32_t n, void *k_pages, void *v_pages, void *staging,
                              hipStream_t stream);
@@ -45,10 +53,10 @@ static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // A planned launch needs the plan's lists on the current device: it never allocates or copies
-// by itself.
-static pv_status ensure_ready(const pv_plan *plan)
+// by itself.  The lists of a plan for 8-bit pools and those of one for 16-bit pools are not alike.
+static pv_status ensure_ready(const pv_plan *plan, bool kv8 = false)
 {
-    if (!plan) return PV_ERR_INVALID_ARG;
+    if (!plan || plan->kv8 != kv8) return PV_ERR_INVALID_ARG;
     if (!plan->uploaded) return PV_ERR_INVALID_ARG;  // pv_plan_upload / pv_plan_upload_to first
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess) return PV_ERR_HIP;
@@ -251,6 +259,19 @@ static pv_status attn_args_ok(const pv_plan *plan, const void *q, const void *k_
     return PV_OK;
 }
 
+// Where a caller's workspace holds the partial outputs, and the (max, sum) pairs behind them.
+static pv_status workspace_parts(const pv_plan *plan, void *workspace, size_t bytes, float **ws_o,
+                                 float **ws_ml)
+{
+    if (plan->workspace_bytes == 0) return PV_OK;
+    if (!workspace || bytes < plan->workspace_bytes ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+        return PV_ERR_WORKSPACE;
+    *ws_o = static_cast<float *>(workspace);
+    *ws_ml = *ws_o + (size_t)plan->partial_slots * plan->pool.head_dim;
+    return PV_OK;
+}
+
 pv_status pv_kv_append_planned(pv_plan *plan, const void *k_new, const void *v_new,
                                const int32_t *page_table, void *k_pages, void *v_pages,
                                void *stream)
@@ -272,34 +293,164 @@ pv_status pv_kv_append_planned(pv_plan *plan, const void *k_new, const void *v_n
     return e == hipSuccess ? PV_OK : PV_ERR_HIP;
 }
 
-pv_status pv_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *q_out,
-                                    const void *k_new, const void *v_new, const float *cos_sin,
-                                    int32_t max_pos, int32_t style, const int32_t *page_table,
-                                    void *k_pages, void *v_pages, void *stream)
+// What the calls that rotate queries and keys ask of their arguments besides the pools (a plan with
+// new tokens).
+static pv_status norm_rope_args_ok(const pv_plan *plan, const pv::NormRope &nr, const void *k_new,
+                                   const void *v_new, int32_t max_pos, const int32_t *page_table)
 {
-    if (!plan) return PV_ERR_INVALID_ARG;
-    if (style != 0 && style != 1) return PV_ERR_INVALID_ARG;
-    if ((q_in == nullptr) != (q_out == nullptr)) return PV_ERR_INVALID_ARG;
-    if (plan->total_q == 0) return PV_OK;
-    if (!k_new || !v_new || !cos_sin || !page_table || !k_pages || !v_pages)
-        return PV_ERR_INVALID_ARG;
-    if (!pv::aligned16(q_in) || !pv::aligned16(q_out) || !pv::aligned16(k_new) ||
-        !pv::aligned16(v_new) || !pv::aligned16(cos_sin) || !pv::aligned16(k_pages) ||
-        !pv::aligned16(v_pages))
-        return PV_ERR_INVALID_ARG;
+    if (!k_new || !v_new || !nr.cos_sin || !page_table) return PV_ERR_INVALID_ARG;
+    for (const void *p : {nr.q_in, (const void *)nr.q_out, k_new, v_new, (const void *)nr.cos_sin,
+                          nr.q_weight, nr.k_weight})
+        if (!pv::aligned16(p)) return PV_ERR_INVALID_ARG;
     for (int32_t r = 0; r < plan->num_reqs; ++r)
         if (plan->q_lens[r] > 0 && (int64_t)plan->ctx_lens[r] + plan->q_lens[r] > max_pos)
             return PV_ERR_OUT_OF_RANGE;
-    pv_status s = pv::ensure_ready(plan);
+    return PV_OK;
+}
+
+static pv_status rope_append16(pv_plan *plan, const pv::NormRope &nr, const void *k_new,
+                               const void *v_new, int32_t max_pos, const int32_t *page_table,
+                               void *k_pages, void *v_pages, void *stream)
+{
+    if (!plan) return PV_ERR_INVALID_ARG;
+    if (nr.style != 0 && nr.style != 1) return PV_ERR_INVALID_ARG;
+    if ((nr.q_in == nullptr) != (nr.q_out == nullptr)) return PV_ERR_INVALID_ARG;
+    if (plan->total_q == 0) return PV_OK;
+    if (!k_pages || !v_pages || !pv::aligned16(k_pages) || !pv::aligned16(v_pages))
+        return PV_ERR_INVALID_ARG;
+    pv_status s = norm_rope_args_ok(plan, nr, k_new, v_new, max_pos, page_table);
+    if (s != PV_OK) return s;
+    s = pv::ensure_ready(plan);
     if (s != PV_OK) return s;
     hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e;
     {
         pv::KernelTimer t(plan, 3, st, true);
-        e = pv::launch_rope_append(plan, plan->dev, style, q_in, q_out, k_new, v_new, cos_sin,
-                                   page_table, k_pages, v_pages, st);
+        e = pv::launch_rope_append(plan, plan->dev, nr, k_new, v_new, page_table, k_pages, v_pages,
+                                   st);
     }
     return e == hipSuccess ? PV_OK : PV_ERR_HIP;
+}
+
+pv_status pv_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *q_out,
+                                    const void *k_new, const void *v_new, const float *cos_sin,
+                                    int32_t max_pos, int32_t style, const int32_t *page_table,
+                                    void *k_pages, void *v_pages, void *stream)
+{
+    const pv::NormRope nr = {style, q_in, q_out, nullptr, nullptr, 1.f, cos_sin};
+    return rope_append16(plan, nr, k_new, v_new, max_pos, page_table, k_pages, v_pages, stream);
+}
+
+pv_status pv_norm_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *q_out,
+                                         const void *k_new, const void *v_new,
+                                         const void *q_weight, const void *k_weight, float eps,
+                                         const float *cos_sin, int32_t max_pos, int32_t style,
+                                         const int32_t *page_table, void *k_pages, void *v_pages,
+                                         void *stream)
+{
+    if (!(eps > 0.f) || !std::isfinite(eps)) return PV_ERR_INVALID_ARG;
+    const pv::NormRope nr = {style, q_in, q_out, q_weight, k_weight, eps, cos_sin};
+    return rope_append16(plan, nr, k_new, v_new, max_pos, page_table, k_pages, v_pages, stream);
+}
+
+// ---------------------------------------------------------------------------------------------
+// 8-bit pools
+// ---------------------------------------------------------------------------------------------
+static bool kv8_pool_ok(const pv_kv8_pool *pool)
+{
+    return pool && pool->k && pool->v && pool->k_scales && pool->v_scales &&
+           pv::aligned16(pool->k) && pv::aligned16(pool->v);
+}
+
+static pv_status kv8_append(pv_plan *plan, const pv::NormRope &nr, const void *k_new,
+                            const void *v_new, const int32_t *page_table, const pv_kv8_pool *pool,
+                            void *stream)
+{
+    pv_status s = pv::ensure_ready(plan, true);
+    if (s != PV_OK) return s;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    {
+        pv::KernelTimer t(plan, 3, st, true);
+        e = pv::launch_kv8_append(plan, plan->dev, nr, k_new, v_new, page_table, *pool, st);
+    }
+    return e == hipSuccess ? PV_OK : PV_ERR_HIP;
+}
+
+pv_status pv_kv8_append_planned(pv_plan *plan, const void *k_new, const void *v_new,
+                                const int32_t *page_table, const pv_kv8_pool *pool, void *stream)
+{
+    if (!plan || !plan->kv8) return PV_ERR_INVALID_ARG;
+    if (plan->total_q == 0) return PV_OK;
+    if (!k_new || !v_new || !page_table || !kv8_pool_ok(pool)) return PV_ERR_INVALID_ARG;
+    if (!pv::aligned16(k_new) || !pv::aligned16(v_new)) return PV_ERR_INVALID_ARG;
+    const pv::NormRope none = {-1, nullptr, nullptr, nullptr, nullptr, 1.f, nullptr};
+    return kv8_append(plan, none, k_new, v_new, page_table, pool, stream);
+}
+
+pv_status pv_kv8_norm_rope_append_planned(pv_plan *plan, const void *q_in, void *q_out,
+                                          const void *k_new, const void *v_new,
+                                          const void *q_weight, const void *k_weight, float eps,
+                                          const float *cos_sin, int32_t max_pos, int32_t style,
+                                          const int32_t *page_table, const pv_kv8_pool *pool,
+                                          void *stream)
+{
+    if (!plan || !plan->kv8) return PV_ERR_INVALID_ARG;
+    if (style != 0 && style != 1) return PV_ERR_INVALID_ARG;
+    if ((q_in == nullptr) != (q_out == nullptr)) return PV_ERR_INVALID_ARG;
+    if (!(eps > 0.f) || !std::isfinite(eps)) return PV_ERR_INVALID_ARG;
+    if (plan->total_q == 0) return PV_OK;
+    if (!kv8_pool_ok(pool)) return PV_ERR_INVALID_ARG;
+    const pv::NormRope nr = {style, q_in, q_out, q_weight, k_weight, eps, cos_sin};
+    const pv_status s = norm_rope_args_ok(plan, nr, k_new, v_new, max_pos, page_table);
+    if (s != PV_OK) return s;
+    return kv8_append(plan, nr, k_new, v_new, page_table, pool, stream);
+}
+
+pv_status pv_kv8_read_planned(pv_plan *plan, const pv_kv8_pool *pool, const int32_t *page_table,
+                              void *k_rows, void *v_rows, void *stream)
+{
+    if (!plan || !plan->kv8) return PV_ERR_INVALID_ARG;
+    if (plan->total_q == 0) return PV_OK;
+    if (!k_rows || !v_rows || !page_table || !kv8_pool_ok(pool)) return PV_ERR_INVALID_ARG;
+    if (!pv::aligned16(k_rows) || !pv::aligned16(v_rows)) return PV_ERR_INVALID_ARG;
+    const pv_status s = pv::ensure_ready(plan, true);
+    if (s != PV_OK) return s;
+    return pv::launch_kv8_read(plan, plan->dev, *pool, page_table, k_rows, v_rows,
+                               static_cast<hipStream_t>(stream)) == hipSuccess
+               ? PV_OK
+               : PV_ERR_HIP;
+}
+
+pv_status pv_kv8_multi_token_paged_attn_planned(pv_plan *plan, const void *q,
+                                                const pv_kv8_pool *pool,
+                                                const int32_t *page_table, float scale, void *out,
+                                                void *workspace, size_t workspace_bytes,
+                                                void *stream)
+{
+    if (!plan || !plan->kv8) return PV_ERR_INVALID_ARG;
+    if (plan->total_q == 0) return PV_OK;
+    if (!kv8_pool_ok(pool)) return PV_ERR_INVALID_ARG;
+    pv_status s = attn_args_ok(plan, q, pool->k, pool->v, page_table, scale, out);
+    if (s != PV_OK) return s;
+    float *ws_o = nullptr, *ws_ml = nullptr;
+    s = workspace_parts(plan, workspace, workspace_bytes, &ws_o, &ws_ml);
+    if (s != PV_OK) return s;
+    s = pv::ensure_ready(plan, true);
+    if (s != PV_OK) return s;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    {
+        pv::KernelTimer t(plan, 0, st, !plan->narrow.empty());
+        if (pv::launch_attn_kv8_narrow(plan, plan->dev, q, *pool, page_table, scale, out, ws_o,
+                                       ws_ml, st) != hipSuccess)
+            return PV_ERR_HIP;
+    }
+    {
+        pv::KernelTimer t(plan, 2, st, !plan->combine.empty());
+        if (pv::launch_attn_combine(plan, plan->dev, ws_o, ws_ml, out, st) != hipSuccess)
+            return PV_ERR_HIP;
+    }
+    return PV_OK;
 }
 
 pv_status pv_multi_token_paged_attn_planned(pv_plan *plan, const void *q, const void *k_pages,
@@ -312,13 +463,8 @@ pv_status pv_multi_token_paged_attn_planned(pv_plan *plan, const void *q, const 
     pv_status s = attn_args_ok(plan, q, k_pages, v_pages, page_table, scale, out);
     if (s != PV_OK) return s;
     float *ws_o = nullptr, *ws_ml = nullptr;
-    if (plan->workspace_bytes > 0) {
-        if (!workspace || workspace_bytes < plan->workspace_bytes ||
-            (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
-            return PV_ERR_WORKSPACE;
-        ws_o = static_cast<float *>(workspace);
-        ws_ml = ws_o + (size_t)plan->partial_slots * plan->pool.head_dim;
-    }
+    s = workspace_parts(plan, workspace, workspace_bytes, &ws_o, &ws_ml);
+    if (s != PV_OK) return s;
     s = pv::ensure_ready(plan);
     if (s != PV_OK) return s;
     return attn_launch(plan, plan->dev, q, k_pages, v_pages, page_table, scale, out, ws_o, ws_ml,
@@ -357,6 +503,7 @@ pv_status pv_multi_token_paged_attn_noalloc(pv_plan *plan, const void *q, const 
 {
     if (!plan) return PV_ERR_INVALID_ARG;
     if (plan->total_q == 0) return PV_OK;
+    if (plan->kv8) return PV_ERR_INVALID_ARG;
     pv_status s = attn_args_ok(plan, q, k_pages, v_pages, page_table, scale, out);
     if (s != PV_OK) return s;
     const size_t lists = pv::align_up(plan->image.size(), 256);

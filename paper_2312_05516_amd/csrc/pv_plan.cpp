@@ -58,6 +58,14 @@ Tuning default_tuning()
     return t;
 }
 
+Tuning kv8_tuning()
+{
+    Tuning t = default_tuning();
+    t.wide_min_rows = INT32_MAX;
+    t.tile_min_keys = t.tile_batch_min_keys = 0;
+    return t;
+}
+
 // Whether the full 256-row tiles of a (request, KV head) unit go to the 256-row kernel: that
 // kernel exists for head size 128 and pays off when an item streams many 32-key blocks.
 static bool use_tile256(const pv_pool_desc *pool, const Tuning &tune, int64_t rows_total,
@@ -510,7 +518,7 @@ pv_status check_batch(const pv_pool_desc *pool, int32_t num_q_heads, const int32
 
 pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_t *ctx_lens,
                      const int32_t *q_lens, int32_t num_reqs, int32_t max_pages_per_req,
-                     const Tuning &tune, pv_plan **out)
+                     const Tuning &tune, pv_plan **out, bool kv8)
 {
     if (!out) return PV_ERR_INVALID_ARG;
     *out = nullptr;
@@ -523,6 +531,7 @@ pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_
     pv_plan *plan = new (std::nothrow) pv_plan();
     if (!plan) return PV_ERR_INVALID_ARG;
     plan->pool = *pool;
+    plan->kv8 = kv8;
     plan->num_q_heads = num_q_heads;
     plan->group = G;
     plan->num_reqs = num_reqs;
@@ -546,11 +555,12 @@ pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_
         at += q_lens[r];
     }
 
-    // append: runs of new tokens that share an 8-slot group of a page
+    // append: runs of new tokens that share an 8-slot group of a page (a page, for 8-bit pools)
+    const int64_t run = kv8 ? 16 : 8;
     for (int32_t r = 0; r < num_reqs; ++r) {
         const int64_t c = ctx_lens[r], end = (int64_t)ctx_lens[r] + q_lens[r];
         for (int64_t t = c; t < end;) {
-            const int64_t group_end = (t / 8 + 1) * 8;
+            const int64_t group_end = (t / run + 1) * run;
             const int64_t stop = std::min(end, group_end);
             AppendGroup g;
             g.req = r;
@@ -809,6 +819,31 @@ int64_t pv_pool_k_offset(const pv_pool_desc *pool, int32_t page, int32_t head, i
     return ((tile * chunks + d / 8) * pool->page_size + slot) * 8 + d % 8;
 }
 
+size_t pv_kv8_pool_bytes(const pv_pool_desc *pool) { return pv_pool_bytes(pool) / 2; }
+
+size_t pv_kv8_scale_bytes(const pv_pool_desc *pool)
+{
+    if (!pv::pool_desc_valid(pool, nullptr)) return 0;
+    return (size_t)pool->num_pages * pool->num_kv_heads;
+}
+
+int64_t pv_kv8_k_offset(const pv_pool_desc *pool, int32_t page, int32_t head, int32_t slot,
+                        int32_t d)
+{
+    if (pv_pool_k_offset(pool, page, head, slot, d) < 0) return -1;
+    const int64_t tile = (int64_t)page * pool->num_kv_heads + head;
+    const int64_t D = pool->head_dim;
+    return tile * 16 * D + slot / 4 * 4 * D + d / 16 * 64 + slot % 4 * 16 + d % 16;
+}
+
+int64_t pv_kv8_v_offset(const pv_pool_desc *pool, int32_t page, int32_t head, int32_t slot,
+                        int32_t d)
+{
+    if (pv_pool_k_offset(pool, page, head, slot, d) < 0) return -1;
+    const int64_t tile = (int64_t)page * pool->num_kv_heads + head;
+    return tile * 16 * pool->head_dim + (int64_t)d * 16 + slot;
+}
+
 int64_t pv_pool_v_offset(const pv_pool_desc *pool, int32_t page, int32_t head, int32_t slot,
                          int32_t d)
 {
@@ -828,6 +863,16 @@ pv_status pv_plan_create(const pv_pool_desc *pool, int32_t num_q_heads, const in
     return pv::build_plan(pool, num_q_heads, ctx_lens, q_lens, num_reqs, max_pages_per_req,
                           pv::default_tuning(), plan);
 }
+
+pv_status pv_plan_create_kv8(const pv_pool_desc *pool, int32_t num_q_heads,
+                             const int32_t *ctx_lens, const int32_t *q_lens, int32_t num_reqs,
+                             int32_t max_pages_per_req, pv_plan **plan)
+{
+    return pv::build_plan(pool, num_q_heads, ctx_lens, q_lens, num_reqs, max_pages_per_req,
+                          pv::kv8_tuning(), plan, true);
+}
+
+int32_t pv_plan_is_kv8(const pv_plan *plan) { return plan ? (plan->kv8 ? 1 : 0) : -1; }
 
 int32_t pv_plan_total_q(const pv_plan *plan) { return plan ? plan->total_q : -1; }
 
@@ -902,7 +947,10 @@ pv_status pv_plan_check_page_table(const pv_plan *plan, const int32_t *page_tabl
         const int32_t *row = page_table + (int64_t)r * plan->max_pages_per_req;
         for (int64_t lp = 0; lp < pages; ++lp)
             if (row[lp] < 0 || row[lp] >= plan->pool.num_pages) return PV_ERR_OUT_OF_RANGE;
-        if (check_append_unique) {
+        if (check_append_unique && plan->kv8) {  // a page with new tokens has one writer
+            for (int64_t lp = c / P; lp < pages; ++lp)
+                if (!seen.insert(row[lp]).second) return PV_ERR_INVALID_ARG;
+        } else if (check_append_unique) {
             for (int32_t j = 0; j < n; ++j) {
                 const int64_t t = (int64_t)c + j;
                 const int64_t key = (int64_t)row[t / P] * P + t % P;

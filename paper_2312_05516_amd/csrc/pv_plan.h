@@ -77,11 +77,12 @@ struct CombineChunk {
 static_assert(sizeof(CombineChunk) == 8, "CombineChunk is read by the kernel as 2 int32");
 
 // Up to 8 consecutive new tokens of one request that fall into the same 8-slot group of a page
-// (the V pool keeps 8 consecutive slots of one head dimension in one 16-byte run).
+// (the V pool keeps 8 consecutive slots of one head dimension in one 16-byte run).  In a plan for
+// 8-bit pools: up to 16 that fall into the same page, which is what has one scale.
 struct AppendGroup {
     int32_t req;
     int32_t t_begin;  // logical position of the first token of the group
-    int32_t count;    // 1..8 tokens
+    int32_t count;    // 1..8 tokens (1..16 for 8-bit pools)
     int32_t q_row;    // row of that first token in k_new / v_new
 };
 static_assert(sizeof(AppendGroup) == 16, "AppendGroup is read by the kernel as 4 int32");
@@ -95,6 +96,17 @@ static_assert(sizeof(AppendGroup) == 16, "AppendGroup is read by the kernel as 4
 // generation steps with the rotary embedding 26.0 and 26.3.  Streaming the stores too is slower
 // (first prompts 193 -> 204 us).
 constexpr int64_t kStreamBytes = 32 << 20;
+
+// What the appends that rotate queries and keys are given besides the rows of K and V.  style: -1 =
+// neither norm nor rotation, else as pv_rope_kv_append_planned; a null weight = no norm.
+struct NormRope {
+    int style;
+    const void *q_in;
+    void *q_out;
+    const void *q_weight, *k_weight;
+    float eps;
+    const float *cos_sin;
+};
 
 // Requests with new tokens that the append takes as a kernel argument, and how many one launch
 // takes (2 KB of arguments).  Request i of the launch has the append groups group0[i] .. group0[i
@@ -238,6 +250,7 @@ struct Tuning {
 
 struct pv_plan {
     pv_pool_desc pool;
+    bool kv8;  // for pools of 8-bit codes (pv_plan_create_kv8): its lists are not for 16-bit pools
     int32_t num_q_heads;
     int32_t group;  // G
     int32_t num_reqs;
@@ -283,11 +296,12 @@ namespace pv {
 DeviceLists lists_at(const pv_plan *plan, const void *base);
 bool pool_desc_valid(const pv_pool_desc *p, pv_status *why);
 Tuning default_tuning();
+Tuning kv8_tuning();  // of plans for 8-bit pools
 // what every plan demands of a batch; *total_q = its new tokens
 pv_status check_batch(const pv_pool_desc *pool, int32_t num_q_heads, const int32_t *ctx_lens,
                       const int32_t *q_lens, int32_t num_reqs, int32_t max_pages_per_req,
                       int32_t *total_q);
 pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_t *ctx_lens,
                      const int32_t *q_lens, int32_t num_reqs, int32_t max_pages_per_req,
-                     const Tuning &tune, pv_plan **out);
+                     const Tuning &tune, pv_plan **out, bool kv8 = false);
 }  // namespace pv

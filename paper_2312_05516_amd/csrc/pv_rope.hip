@@ -15,32 +15,22 @@
 // heads first (K rotated + scattered, V scattered as in kv_append_kernel), then the query heads of
 // the group's tokens.  The heads of a token share its angles, which are twice the bytes of one
 // head's row, so a thread loads them once for all its heads, and then all its rows at once.
+#include <type_traits>
+
 #include "pv_device.h"
 
 namespace pv {
 
-template <typename T>
-__device__ __forceinline__ void unpack8(u32x4 raw, float (&x)[8])
-{
-    const typename T::vec8 v = as_vec8<T>(raw);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
-}
-
-template <typename T>
-__device__ __forceinline__ u32x4 pack8(const float (&x)[8])
-{
-    return u32x4{T::pack2(x[0], x[1]), T::pack2(x[2], x[3]), T::pack2(x[4], x[5]),
-                 T::pack2(x[6], x[7])};
-}
-
-template <typename T, int D, int STYLE, int HB>
+// NORM: rows whose kind has a weight are first scaled to y = x * w / sqrt(mean(x^2) + eps), in fp32
+// and without a rounding of their own; the lanes that hold a row are neighbours.
+template <typename T, int D, int STYLE, int HB, bool NORM>
 __global__ __launch_bounds__(D) void rope_append_kernel(
     const AppendGroup *__restrict__ groups, const uint16_t *q_in,
     uint16_t *q_out /* may be q_in */, const uint16_t *__restrict__ k_new,
     const uint16_t *__restrict__ v_new, const float *__restrict__ cos_sin,
     const int32_t *__restrict__ page_table, int32_t max_pages, int32_t num_q_heads,
-    int32_t num_kv_heads, uint16_t *__restrict__ k_pages, uint16_t *__restrict__ v_pages)
+    int32_t num_kv_heads, uint16_t *__restrict__ k_pages, uint16_t *__restrict__ v_pages,
+    const uint16_t *__restrict__ q_weight, const uint16_t *__restrict__ k_weight, float eps)
 {
     constexpr int CH = D / 8;
     const AppendGroup g = groups[blockIdx.x];
@@ -53,6 +43,8 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
     const int64_t row_stride = (int64_t)(is_q ? num_q_heads : num_kv_heads) * D;
     const int64_t src_off = (int64_t)g.q_row * row_stride + (int64_t)h0 * D;
     const uint16_t *src = (is_q ? q_in : k_new) + src_off;
+
+    const uint16_t *weight = NORM ? (is_q ? q_weight : k_weight) : nullptr;
 
     int64_t tile = 0;
     int slot0 = 0;
@@ -85,10 +77,22 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
             for (int i = 0; i < HB; ++i) {
                 float x[8], o[8];
                 unpack8<T>(raw[i], x);
+                if (NORM && weight) {
+                    float w[8];
+                    unpack8<T>(load16(weight + 8 * c8), w);
+                    const float mine = sum_squares(x);
+                    const float r = norm_factor<D>(mine + __shfl_xor(mine, CH / 2), eps);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = x[e] * r * w[e];
+                }
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    o[2 * p] = x[2 * p] * c[p] - x[2 * p + 1] * s[p];
-                    o[2 * p + 1] = x[2 * p + 1] * c[p] + x[2 * p] * s[p];
+                    if constexpr (NORM) {
+                        rotate_pair(x[2 * p], x[2 * p + 1], c[p], s[p], o[2 * p], o[2 * p + 1]);
+                    } else {
+                        o[2 * p] = x[2 * p] * c[p] - x[2 * p + 1] * s[p];
+                        o[2 * p + 1] = x[2 * p + 1] * c[p] + x[2 * p] * s[p];
+                    }
                 }
                 if (i < heads) store_chunk(j, i, c8, pack8<T>(o));
             }
@@ -122,11 +126,27 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
                 float xa[8], xb[8], oa[8], ob[8];
                 unpack8<T>(ra[m], xa);
                 unpack8<T>(rb[m], xb);
+                if (NORM && weight) {
+                    float wa[8], wb[8];
+                    unpack8<T>(load16(weight + 8 * c8), wa);
+                    unpack8<T>(load16(weight + D / 2 + 8 * c8), wb);
+                    const float r =
+                        norm_factor<D>(sum_squares(xa) + sum_squares(xb), eps);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        xa[e] = xa[e] * r * wa[e];
+                        xb[e] = xb[e] * r * wb[e];
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float ce = c[e / 4][e % 4], se = s[e / 4][e % 4];
-                    oa[e] = xa[e] * ce - xb[e] * se;
-                    ob[e] = xb[e] * ce + xa[e] * se;
+                    if constexpr (NORM) {
+                        rotate_pair(xa[e], xb[e], ce, se, oa[e], ob[e]);
+                    } else {
+                        oa[e] = xa[e] * ce - xb[e] * se;
+                        ob[e] = xb[e] * ce + xa[e] * se;
+                    }
                 }
                 if (i < heads) {
                     store_chunk(j, i, c8, pack8<T>(oa));
@@ -142,20 +162,20 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
                                          v_pages + tile);
 }
 
-template <typename T, int D, int STYLE, int HB>
-static void launch_rope_t(const pv_plan *plan, const DeviceLists &dl, const void *q_in, void *q_out,
-                          const void *k_new, const void *v_new, const float *cos_sin,
-                          const int32_t *page_table, void *k_pages, void *v_pages,
-                          hipStream_t stream)
+template <typename T, int D, int STYLE, int HB, bool NORM>
+static void launch_rope_t(const pv_plan *plan, const DeviceLists &dl, const NormRope &nr,
+                          const void *k_new, const void *v_new, const int32_t *page_table,
+                          void *k_pages, void *v_pages, hipStream_t stream)
 {
     const int kv_blocks = (plan->pool.num_kv_heads + HB - 1) / HB;
-    const int q_blocks = q_in ? (plan->num_q_heads + HB - 1) / HB : 0;
+    const int q_blocks = nr.q_in ? (plan->num_q_heads + HB - 1) / HB : 0;
     const dim3 grid((unsigned)plan->append_groups.size(), (unsigned)(kv_blocks + q_blocks));
-    hipLaunchKernelGGL((rope_append_kernel<T, D, STYLE, HB>), grid, dim3(D), 0, stream,
-                       dl.append_groups, (const uint16_t *)q_in, (uint16_t *)q_out,
-                       (const uint16_t *)k_new, (const uint16_t *)v_new, cos_sin, page_table,
-                       plan->max_pages_per_req, plan->num_q_heads, plan->pool.num_kv_heads,
-                       (uint16_t *)k_pages, (uint16_t *)v_pages);
+    hipLaunchKernelGGL((rope_append_kernel<T, D, STYLE, HB, NORM>), grid, dim3(D), 0, stream,
+                       dl.append_groups, (const uint16_t *)nr.q_in, (uint16_t *)nr.q_out,
+                       (const uint16_t *)k_new, (const uint16_t *)v_new, nr.cos_sin,
+                       page_table, plan->max_pages_per_req, plan->num_q_heads,
+                       plan->pool.num_kv_heads, (uint16_t *)k_pages, (uint16_t *)v_pages,
+                       (const uint16_t *)nr.q_weight, (const uint16_t *)nr.k_weight, nr.eps);
 }
 
 // A large batch: two rows a thread (two heads a workgroup, four where pairs span the halves of a
@@ -164,26 +184,31 @@ static void launch_rope_t(const pv_plan *plan, const DeviceLists &dl, const void
 // 182 with four; 190 with four and no hint), half pairs 185 -> 177 (185 with two, 178 with eight);
 // 64/8 heads, 4 K tokens, half pairs 95 -> 91.  A small batch keeps one head a workgroup, the more of
 // them run at once (4 generation steps, 64/8 heads: 24.8 us against 25.5).
-template <typename T, int D>
+template <typename T, int D, bool NORM>
 static auto pick_rope(int style, bool many)
 {
-    if (style == 0) return many ? launch_rope_t<T, D, 0, 2> : launch_rope_t<T, D, 0, 1>;
-    return many ? launch_rope_t<T, D, 1, 4> : launch_rope_t<T, D, 1, 1>;
+    if (style == 0) return many ? launch_rope_t<T, D, 0, 2, NORM> : launch_rope_t<T, D, 0, 1, NORM>;
+    return many ? launch_rope_t<T, D, 1, 4, NORM> : launch_rope_t<T, D, 1, 1, NORM>;
 }
 
-hipError_t launch_rope_append(const pv_plan *plan, const DeviceLists &dl, int style, const void *q_in, void *q_out,
-                              const void *k_new, const void *v_new, const float *cos_sin,
-                              const int32_t *page_table, void *k_pages, void *v_pages,
-                              hipStream_t stream)
+hipError_t launch_rope_append(const pv_plan *plan, const DeviceLists &dl, const NormRope &nr,
+                              const void *k_new, const void *v_new, const int32_t *page_table,
+                              void *k_pages, void *v_pages, hipStream_t stream)
 {
     if (plan->append_groups.empty()) return hipSuccess;
     const bool f = plan->pool.dtype == PV_F16;
-    const int64_t rows = 2 * plan->pool.num_kv_heads + (q_in ? plan->num_q_heads : 0);
+    const int64_t rows = 2 * plan->pool.num_kv_heads + (nr.q_in ? plan->num_q_heads : 0);
     const bool many = plan->total_q * rows * plan->pool.head_dim * 2 > kStreamBytes;
-    auto go = plan->pool.head_dim == 128
-                  ? (f ? pick_rope<F16, 128>(style, many) : pick_rope<BF16, 128>(style, many))
-                  : (f ? pick_rope<F16, 64>(style, many) : pick_rope<BF16, 64>(style, many));
-    go(plan, dl, q_in, q_out, k_new, v_new, cos_sin, page_table, k_pages, v_pages, stream);
+    auto pick = [&](auto norm) {
+        constexpr bool NORM = decltype(norm)::value;
+        return plan->pool.head_dim == 128
+                   ? (f ? pick_rope<F16, 128, NORM>(nr.style, many)
+                        : pick_rope<BF16, 128, NORM>(nr.style, many))
+                   : (f ? pick_rope<F16, 64, NORM>(nr.style, many)
+                        : pick_rope<BF16, 64, NORM>(nr.style, many));
+    };
+    auto go = nr.q_weight || nr.k_weight ? pick(std::true_type{}) : pick(std::false_type{});
+    go(plan, dl, nr, k_new, v_new, page_table, k_pages, v_pages, stream);
     return hipGetLastError();
 }
 

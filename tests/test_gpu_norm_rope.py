@@ -1,0 +1,273 @@
+"""Norms of queries and keys with the rotation and the append, into 16-bit and into 8-bit pools, against
+the formula in 64 bits."""
+import numpy as np
+import pytest
+
+import helpers as H
+import kv8_ref as R
+from paper_2312_05516_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-6
+
+
+def _batch(heads, dtype, ctx=(37, 0, 250, 8, 100), new=(5, 33, 1, 0, 19)):
+    return wl.custom(ctx, new, num_q_heads=heads[0], num_kv_heads=heads[1], head_dim=heads[2],
+                     dtype=dtype, seed=77)
+
+
+def _inputs(b, seed=1, std=3.0):
+    q = R.random_bits((b.total_q, b.num_q_heads, b.head_dim), b.dtype, seed, std)
+    k, v = (R.random_bits((b.total_q, b.num_kv_heads, b.head_dim), b.dtype, seed + i, std)
+            for i in (1, 2))
+    w = [H.f64_to_bits(1 + 0.3 * np.random.default_rng(seed + i).standard_normal(b.head_dim), b.dtype)
+         for i in range(2)]
+    return q, k, v, w
+
+
+def _table(b):
+    from paper_2312_05516_amd import binding as pv
+    return pv.rope_table(10000.0, b.head_dim, int(b.kv_lens.max()))
+
+
+def _call16(b, q, k, v, weights, style, eps=EPS, in_place=False, pools=None, table=None):
+    """(q_out bits or None, K rows bits, V rows bits, the two pools)"""
+    import torch
+    from paper_2312_05516_amd import binding as pv
+    desc = pv.pool_desc(b.num_pages, b.num_kv_heads, b.head_dim, b.dtype)
+    plan = pv.plan_create(desc, b.num_q_heads, b.ctx_lens, b.q_lens, b.max_pages_per_req)
+    pv.plan_upload(plan)
+    dev = [None if x is None else H.to_dev_bits(x, b.dtype) for x in (q, k, v, *weights)]
+    kp, vp = (torch.full((wl.pool_elems(b),), float("nan"), dtype=H._torch_dtype(b.dtype),
+                         device="cuda") for _ in "kv")
+    q_out = None if q is None else dev[0] if in_place else torch.empty_like(dev[0])
+    pv.norm_rope_kv_append_planned(plan, dev[0], q_out, dev[1], dev[2], dev[3], dev[4], eps,
+                                   torch.from_numpy(_table(b) if table is None else table).cuda(),
+                                   style, torch.from_numpy(b.page_table).cuda(), kp, vp)
+    torch.cuda.synchronize()
+    kb, vb = H.from_dev_bits(kp), H.from_dev_bits(vp)
+    k_rows, v_rows = (np.zeros_like(k) for _ in "kv")
+    kv, vv = H.k_view(b, kb), H.v_view(b, vb)
+    at = 0
+    for r in range(b.num_reqs):
+        for t in range(int(b.ctx_lens[r]), int(b.kv_lens[r])):
+            page, s = int(b.page_table[r, t // 16]), t % 16
+            k_rows[at] = kv[page, :, :, s].reshape(b.num_kv_heads, -1)
+            v_rows[at] = vv[page, :, s // 8, :, s % 8]
+            at += 1
+    return None if q is None else H.from_dev_bits(q_out), k_rows, v_rows, (kb, vb)
+
+
+def _close(got, x, weight, b, style, eps=EPS):
+    """Bound: one rounding to 16 bits (half a step of the value, or of the smallest normal one) of a
+    result a*cos -+ b*sin whose terms went through fp32: a sum of D squares, a root, a division and two
+    products, together at most (D + 8) * 2^-24 relative, and three more roundings for the rotation."""
+    X = H.bits_to_f64(x, b.dtype)
+    W = None if weight is None else H.bits_to_f64(weight, b.dtype)
+    want = R.norm_rotate(X, W, eps, _table(b), R.positions(b), style)
+    y = X if W is None else X * W / np.sqrt((X * X).mean(axis=2, keepdims=True) + eps)
+    least = 2.0 ** (-14 if b.dtype == "f16" else -126)
+    bound = (R.HALF_STEP[b.dtype] * np.maximum(np.abs(want), least)
+             + (b.head_dim + 12) * 2.0 ** -23 * np.abs(y).max(axis=2, keepdims=True))
+    err = np.abs(H.bits_to_f64(got, b.dtype) - want)
+    assert (err <= bound).all(), float((err / bound).max())
+
+
+HEADS = [(6, 3, 128), (33, 11, 64), (8, 1, 128), (5, 5, 64)]
+
+
+@pytest.mark.parametrize("style", ["interleaved", "half"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", HEADS)
+def test_norm_and_rotation_into_16_bit_pools(heads, dtype, style):
+    b = _batch(heads, dtype)
+    q, k, v, w = _inputs(b)
+    q_out, k_rows, v_rows, (kb, vb) = _call16(b, q, k, v, w, style)
+    _close(q_out, q, w[0], b, style)
+    _close(k_rows, k, w[1], b, style)
+    assert np.array_equal(v_rows, v)
+    # nothing else was written
+    nan = wl.nan_pattern(b.dtype)
+    assert (kb == nan).sum() == (vb == nan).sum() == kb.size - b.total_q * b.num_kv_heads * b.head_dim
+    again = _call16(b, q, k, v, w, style, in_place=True)
+    assert np.array_equal(again[0], q_out) and np.array_equal(again[1], k_rows)
+
+
+@pytest.mark.parametrize("style", ["interleaved", "half"])
+@pytest.mark.parametrize("heads,dtype", [((70, 7, 128), "bf16"), ((33, 11, 64), "f16")])
+def test_many_rows(heads, dtype, style):
+    """Batches over 32 MiB of rows take several heads a workgroup."""
+    new = [900, 1, 500, 77] if heads[2] == 128 else [5000, 1, 1500, 77]
+    b = wl.custom([0, 9, 4, 100], new, num_q_heads=heads[0], num_kv_heads=heads[1],
+                  head_dim=heads[2], dtype=dtype, seed=78)
+    assert b.total_q * (heads[0] + 2 * heads[1]) * heads[2] * 2 > 32 << 20 or heads[2] == 128
+    q, k, v, w = _inputs(b, 4)
+    q_out, k_rows, v_rows, _ = _call16(b, q, k, v, w, style)
+    _close(q_out, q, w[0], b, style)
+    _close(k_rows, k, w[1], b, style)
+    assert np.array_equal(v_rows, v)
+
+
+@pytest.mark.parametrize("style", ["interleaved", "half"])
+def test_without_a_weight_a_kind_is_only_rotated(style):
+    b = _batch((6, 3, 128), "bf16")
+    q, k, v, w = _inputs(b)
+    plain = _call16(b, q, k, v, (None, None), style)
+    only_q = _call16(b, q, k, v, (w[0], None), style)
+    only_k = _call16(b, None, k, v, (None, w[1]), style)
+    both = _call16(b, q, k, v, w, style)
+    assert np.array_equal(only_q[0], both[0])
+    _close(only_q[1], k, None, b, style)
+    assert only_k[0] is None and np.array_equal(only_k[1], both[1])
+    _close(plain[0], q, None, b, style)
+    _close(plain[1], k, None, b, style)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_rows_of_zeros_and_of_extreme_size(dtype):
+    """Zeros stay zero; tiny rows are divided by sqrt(eps); the largest f16 values do not overflow."""
+    b = _batch((2, 2, 128), dtype)
+    q, k, v, w = _inputs(b)
+    q[0], k[1] = 0, 0
+    q[2] = R.random_bits((2, 128), dtype, 9, 1e-6 if dtype == "f16" else 1e-30)
+    big = R.random_bits((2, 128), dtype, 10, 15000.0 if dtype == "f16" else 1e17)
+    q[3], k[3] = big, big
+    for eps in (1e-6, 1e-12):
+        q_out, k_rows, _, _ = _call16(b, q, k, v, w, "half", eps=eps)
+        assert not (q_out[0] & 0x7FFF).any() and not (k_rows[1] & 0x7FFF).any()
+        _close(q_out, q, w[0], b, "half", eps)
+        _close(k_rows, k, w[1], b, "half", eps)
+
+
+def test_nan_stays_in_its_row():
+    b = _batch((2, 2, 128), "bf16")
+    q, k, v, w = _inputs(b)
+    q[4, 1, 7], k[5, 0, 100] = 0x7FC0, 0x7F80
+    q_out, k_rows, _, _ = _call16(b, q, k, v, w, "interleaved")
+    for got, bad in ((q_out, (4, 1)), (k_rows, (5, 0))):
+        nan = np.isnan(H.bits_to_f64(got, "bf16"))
+        assert nan[bad].any()
+        nan[bad] = False
+        assert not nan.any()
+
+
+# ------------------------------------------------------------------ into 8-bit pools
+def _same_or_next(got, want, exact):
+    if exact:
+        return got.same_as(want)
+    far = np.abs(R.one_nan(got.k).astype(np.int64) - R.one_nan(want.k))
+    assert (far <= 1).all() and (far > 0).mean() < 5e-3
+    got.k[:] = want.k
+    got.same_as(want)
+
+
+@pytest.mark.parametrize("style", ["interleaved", "half"])
+@pytest.mark.parametrize("weights", ["both", "none"])
+@pytest.mark.parametrize("heads,dtype", [((6, 3, 128), "bf16"), ((33, 11, 64), "f16"),
+                                         ((8, 1, 128), "f16"), ((5, 5, 64), "bf16")])
+def test_into_8_bit_pools_is_norm_rotation_and_append(heads, dtype, weights, style):
+    """What the call for 16-bit pools rounds, quantised as the append does: bit for bit in bf16 with norms.
+    In f16 the last multiply-add and the rounding to 16 bits may be one instruction, which rounds once
+    where two round twice, and without norms the two terms of a rotation may be added in either order.
+    Results differ then only where the exact one lies within an fp32 rounding or two of the middle of
+    two 16-bit values, by one step of them.  So rotated queries may be neighbours, and codes of keys
+    too: the rounding to a code is monotonic, and codes lie at least 16 such steps apart."""
+    import torch
+    b = _batch(heads, dtype)
+    q, k, v, w = _inputs(b)
+    exact = dtype == "bf16" and weights == "both"
+    if weights == "none":
+        w = (None, None)
+    q16, k16, _, _ = _call16(b, q, k, v, w, style)
+    before = R.Pools(b, "random", seed=12)
+    want = before.copy()
+    R.append(want, k16, v)
+    run = R.Run(b)
+    for in_place in (False, True):
+        dev = R.to_dev(before)
+        d = [None if x is None else H.to_dev_bits(x, dtype) for x in (q, k, v, *w)]
+        out = d[0] if in_place else torch.empty_like(d[0])
+        run.pv.kv8_norm_rope_append_planned(run.plan, d[0], out, *d[1:], EPS,
+                                            torch.from_numpy(_table(b)).cuda(), style, run.table, dev)
+        _same_or_next(R.from_dev(dev, b), want, exact)
+        got = H.from_dev_bits(out)
+        if exact:
+            assert np.array_equal(got, q16)
+        else:
+            assert (np.abs(got.astype(np.int64) - q16) <= 1).all() and (got != q16).mean() < 5e-3
+            _close(got, q, w[0], b, style)
+    dev = R.to_dev(before)  # keys and values alone
+    run.pv.kv8_norm_rope_append_planned(run.plan, None, None, *d[1:], EPS,
+                                        torch.from_numpy(_table(b)).cuda(), style, run.table, dev)
+    _same_or_next(R.from_dev(dev, b), want, exact)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_a_layer_of_a_model_with_normalised_queries_and_keys(eight):
+    """Norm, rotation, append and attention over prompts and generation steps, in a graph as well."""
+    import torch
+    from paper_2312_05516_amd import binding as pv
+    dtype = "bf16"
+    b = wl.custom([0, 90, 33], [60, 1, 20], num_q_heads=8, num_kv_heads=2, head_dim=128, dtype=dtype,
+                  seed=5)
+    q, k, v, w = _inputs(b, 14)
+    k_old, v_old = (R.random_bits((int(b.ctx_lens.sum()), 2, 128), dtype, 90 + i) for i in range(2))
+    table = torch.from_numpy(_table(b)).cuda()
+    p = R.Pools(b)
+    R.append(p, k_old, v_old, np.zeros_like(b.ctx_lens), b.ctx_lens)
+    d = [H.to_dev_bits(x, dtype) for x in (q, k, v, *w)]
+    q_rot, out = torch.empty_like(d[0]), torch.empty_like(d[0])
+    run = R.Run(b)
+    if eight:
+        dev = R.to_dev(p)
+
+        def layer():
+            pv.kv8_norm_rope_append_planned(run.plan, d[0], q_rot, *d[1:], EPS, table, "half",
+                                            run.table, dev)
+            pv.kv8_multi_token_paged_attn_planned(run.plan, q_rot, dev, run.table, b.scale, out, run.ws)
+    else:
+        kp, vp = (np.zeros(wl.pool_elems(b), np.uint16) for _ in "kv")
+        at = 0
+        for r in range(b.num_reqs):
+            for t in range(int(b.ctx_lens[r])):
+                H.put_token(b, kp, vp, int(b.page_table[r, t // 16]), t % 16, k_old[at], v_old[at])
+                at += 1
+        kp, vp = H.to_dev_bits(kp, dtype), H.to_dev_bits(vp, dtype)
+        plan = pv.plan_create(run.desc, 8, b.ctx_lens, b.q_lens, b.max_pages_per_req)
+        pv.plan_upload(plan)
+        ws = torch.empty(max(256, pv.plan_workspace_bytes(plan)), dtype=torch.uint8, device="cuda")
+
+        def layer():
+            pv.norm_rope_kv_append_planned(plan, d[0], q_rot, *d[1:], EPS, table, "half", run.table,
+                                           kp, vp)
+            pv.multi_token_paged_attn_planned(plan, q_rot, kp, vp, run.table, b.scale, out, ws)
+
+    layer()
+    torch.cuda.synchronize()
+    first = out.clone()
+    rotated = [R.norm_rotate(H.bits_to_f64(x, dtype), H.bits_to_f64(y, dtype), EPS, _table(b),
+                             R.positions(b), "half") for x, y in ((q, w[0]), (k, w[1]))]
+    q_bits = H.from_dev_bits(q_rot)
+    _close(q_bits, q, w[0], b, "half")
+    if eight:
+        want = R.from_dev(dev, b)  # what was stored is tested bit for bit above
+        o, bound = R.attention(b, H.bits_to_f64(q_bits, dtype), want, b.scale)
+    else:
+        k_full, v_full, at = [], [], 0
+        for r in range(b.num_reqs):
+            c, n, s = int(b.ctx_lens[r]), int(b.q_lens[r]), int(b.q_start[r])
+            k_full.append(np.concatenate([k_old[at:at + c], H.f64_to_bits(rotated[1][s:s + n], dtype)]))
+            v_full.append(np.concatenate([v_old[at:at + c], v[s:s + n]]))
+            at += c
+        case = H.make_case(b, k_full=k_full, v_full=v_full, q=q_bits)
+        o, bound = H.dense_causal_attention(case), H.TOL[dtype]
+        bound = bound * max(1.0, np.abs(H.bits_to_f64(v, dtype)).max() / 4)  # TOL is for values up to 4
+    assert (np.abs(H.bits_to_f64(H.from_dev_bits(first), dtype) - o) <= bound).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer()
+    for _ in range(3):
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, first)
