@@ -34,7 +34,7 @@
 // loops were split and the operands requested ahead 262.7 and 102.7.
 #include <type_traits>
 
-#include "pv_device.h"
+#include "pv_kv8.h"
 
 namespace pv {
 
@@ -42,15 +42,19 @@ namespace pv {
 // hint (see kStreamKvBytes).
 // RENEW: some item has renew_blocks.  Lists without any keep an instantiation of their own: with the
 // test for it in the loop they take 1 % longer.
-template <typename T, int D, bool RENEW, bool STREAMS>
+// KV8: the pools hold 8-bit codes (pv_kv8.h).  Their blocks go through registers: every thread reads 16
+// codes of K and 16 of V, a block ahead, and stores them widened to 16 bits in LDS, in the layout that
+// the copies of 16-bit pages have there, so that a code is converted once for all rows of the item.
+template <typename T, int D, bool RENEW, bool STREAMS, bool KV8>
 __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
     const WorkItem *__restrict__ items, const uint16_t *__restrict__ q,
     const uint16_t *__restrict__ k_pages, const uint16_t *__restrict__ v_pages,
     const int32_t *__restrict__ page_table, int32_t max_pages, int32_t num_q_heads,
     int32_t num_kv_heads, int32_t group, float scale_log2e, uint32_t q_keep, uint32_t q_sign,
     uint16_t *__restrict__ out, float *__restrict__ ws_o, float *__restrict__ ws_ml,
-    int32_t num_reqs)
+    int32_t num_reqs, const uint8_t *__restrict__ k_scales, const uint8_t *__restrict__ v_scales)
 {
+    static_assert(!(KV8 && STREAMS), "no such instance");
     // Keys per block: 32 for head size 128; 64 for head size 64, where 32 keys are only 8
     // matrix-core instructions of a wavefront against about 70 of the vector ALU, a barrier, a
     // test for the maximum and two LDS round trips.  48 requests over 0.1-3 K tokens, 32/8 heads:
@@ -65,6 +69,9 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
     constexpr int HALF_BYTES = PAGES * TILE_BYTES;  // K (or V) part of a stage
     constexpr int PASSES = HALF_BYTES / 4096;   // 16-byte copies per lane for K (same for V)
     constexpr int STAGES = 3;
+    // operands of V that are requested while the scores are computed
+    constexpr int V_AHEAD = KV8 && D == 128 ? 6 : PAGES * NB;
+    constexpr int K_AHEAD = KV8 && D == 128 ? 6 : 64;  // and of K before the first product
     typedef typename T::vec8 vec8;
     __shared__ __attribute__((aligned(16))) unsigned char smem[STAGES][2 * HALF_BYTES];
 
@@ -182,7 +189,7 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
         constexpr bool MASKED = decltype(masked_tag)::value;
         u32x4 kf[NT * KS];  // K operands, requested as soon as the block is published
 #pragma unroll
-        for (int i = 0; i < NT * KS; ++i)
+        for (int i = 0; i < (K_AHEAD < NT * KS ? K_AHEAD : NT * KS); ++i)
             kf[i] = *reinterpret_cast<const u32x4 *>(sb + k_lds + (i / KS) * 2 * TILE_BYTES +
                                                      (i % KS) * 512);
         f32x16 s[NT];
@@ -193,16 +200,26 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+            for (int ks = 0; ks < KS; ++ks) {
                 s[t] = T::mfma32(as_vec8<T>(kf[t * KS + ks]), qf[ks], s[t]);
+                if (t * KS + ks + K_AHEAD < NT * KS) {
+                    const int i = t * KS + ks + K_AHEAD;
+                    __builtin_amdgcn_sched_barrier(0);
+                    kf[i] = *reinterpret_cast<const u32x4 *>(sb + k_lds + (i / KS) * 2 * TILE_BYTES +
+                                                             (i % KS) * 512);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         // all V operands are requested while the matrix cores work on the scores, so that they have
         // arrived when the first exponentials are done
         __builtin_amdgcn_sched_barrier(0);
         u32x4 vf[PAGES * NB];
-#pragma unroll
-        for (int i = 0; i < PAGES * NB; ++i)
+        auto request_v = [&](int i) {
             vf[i] = *reinterpret_cast<const u32x4 *>(sb + v_lds + (i / NB) * TILE_BYTES +
                                                      (i % NB) * 512);
+        };
+#pragma unroll
+        for (int i = 0; i < V_AHEAD; ++i) request_v(i);
         __builtin_amdgcn_sched_barrier(0);
         // register v = 8*page + j of tile t  <->  key kb0 + 32*t + 16*page + 8*h + j
         if constexpr (MASKED) {
@@ -262,8 +279,71 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
 #pragma unroll
             for (int blk = 0; blk < NB; ++blk)
                 o[blk] = T::mfma32(as_vec8<T>(vf[pg * NB + blk]), pf, o[blk]);
+            if constexpr (V_AHEAD < PAGES * NB) {
+                if (pg == 0) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = V_AHEAD; i < PAGES * NB; ++i) request_v(i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
         l_run += psum;
+    };
+
+    // KV8: the page of a block that this wavefront's threads read, and which 16 codes of it each; the
+    // slots of a chunk of K are neighbouring lanes, whose stores to LDS then lie side by side
+    constexpr int PAGE_THREADS = 256 / PAGES;
+    static_assert(!KV8 || PAGE_THREADS == D, "a thread reads 16 codes of K and of V");
+    const int my_page = w * 64 / PAGE_THREADS;
+    // below it nothing is masked for any row of the item
+    const int item_unmasked = min(it.ctx + (int)rows.tok0 + 1, it.kv_end);
+    __shared__ int left_out;
+    if (KV8 && threadIdx.x == 0) left_out = 0;
+    u32x4 k8, v8;
+    uint32_t k8_scale, v8_scale;
+    auto page_id8 = [&](int b) {
+        const int pg = pg0 + PAGES * b + my_page;
+        return pt[pg <= last_pg ? pg : last_pg];
+    };
+    // the thread's place in the page, worked out anew for each block: there is no register to keep it in
+    auto in_page = [&]() {
+        int l = (int)lane_bytes;
+        asm volatile("" : "+v"(l));
+        return (w * 64 % PAGE_THREADS) + (l >> 4);
+    };
+    auto load8 = [&](int id) {
+        const int at = in_page();
+        const int64_t tile = (int64_t)id * num_kv_heads + it.kv_head;
+        const uint8_t *k_from = reinterpret_cast<const uint8_t *>(k_pages) + tile * (16 * D);
+        const uint8_t *v_from = reinterpret_cast<const uint8_t *>(v_pages) + tile * (16 * D);
+        k8 = load16(k_from + (uint32_t)kv8_k_chunk<D>(at % 16, at / 16));
+        v8 = load16(v_from + (uint32_t)(at * 16));
+        k8_scale = k_scales[tile];
+        v8_scale = v_scales[tile];
+    };
+    // block b, whose codes were loaded before, into the stage
+    auto widen8 = [&](unsigned char *stage, int b) {
+        const int at = in_page();
+        if (it.kv_begin + BK * (b + 1) > item_unmasked) {
+            // A NaN among values that some row does not see: zero times it would be NaN in that row too.
+            // It is left out, and given to the rows that see it at the end.
+            uint32_t any = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t nan = nan_codes(v8[i]);
+                any |= nan;
+                v8[i] &= ~((nan >> 7) * 0xFFu);
+            }
+            if (any) left_out = 1;
+        }
+        const float ks = exp2_scale((int)k8_scale), vs = exp2_scale((int)v8_scale);
+        u32x4 *k_to = reinterpret_cast<u32x4 *>(stage + my_page * TILE_BYTES) + (at / 16 * 32 + at % 16);
+        u32x4 *v_to = reinterpret_cast<u32x4 *>(stage + HALF_BYTES + my_page * TILE_BYTES) + at;
+        k_to[0] = decode8<T>(k8[0], k8[1], ks);
+        k_to[16] = decode8<T>(k8[2], k8[3], ks);
+        v_to[0] = decode8<T>(v8[0], v8[1], vs);
+        v_to[D] = decode8<T>(v8[2], v8[3], vs);
     };
 
     // prologue: blocks 0 and 1 on their way, block 0 landed and visible to everyone; the page ids of
@@ -275,6 +355,17 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
         else
             dma_block(stage, id0, id1, std::false_type{});
     };
+    if constexpr (KV8) {
+        load8(page_id8(0));
+        id0 = page_id8(1);
+        id1 = page_id8(2);
+        __builtin_amdgcn_s_barrier();  // left_out is cleared
+        widen8(smem[0], 0);
+        load8(id0);
+        id0 = id1;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+    } else {
     page_ids(0, id0, id1);
     dma_first(smem[0]);
     if (nblocks > 1) {
@@ -290,6 +381,7 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
         __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
     __builtin_amdgcn_s_barrier();
     asm volatile("" : "+s"(id0), "+s"(id1)::"memory");
+    }
 
     // The item's blocks; `stream`: with the streaming hint on its copies from the third block on.  A
     // flow of its own for either: with both kinds of copies in one loop and a branch between them
@@ -300,6 +392,19 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
         // one block: `compute` works on its stage between the copy of the block after next and the
         // barrier that publishes the next one
         auto step = [&](int b, auto compute) {
+            if constexpr (KV8) {
+                if constexpr (RENEW) to_renewal = (to_renewal == 0 ? renew_blocks : to_renewal) - 1;
+                compute(smem[at], it.kv_begin + BK * b);
+                __builtin_amdgcn_sched_barrier(0);
+                at ^= 1;
+                widen8(smem[at], b + 1);  // where everyone is done with block b - 1
+                load8(id0);        // block b + 2
+                id0 = page_id8(b + 3);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" : "+s"(id0)::"memory");
+                return;
+            }
             const bool more = b + 2 < nblocks;
             if (more) dma_block(smem[at2], id0, id1, stream);  // everyone is done with block b-1
             if constexpr (RENEW) to_renewal = (to_renewal == 0 ? renew_blocks : to_renewal) - 1;
@@ -355,6 +460,39 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
         run(std::bool_constant<STREAMS>{});
     else
         run(std::false_type{});
+
+    if constexpr (KV8) {
+        // NaNs that were left out: counted for each row and dimension by one more product, of ones in
+        // their places with ones for the keys that a row sees
+        if (left_out) {
+            const int l = (int)(lane_bytes >> 4);
+#pragma unroll 1
+            for (int pg = max(item_unmasked - it.kv_begin, 0) / BK * PAGES; pg <= last_pg - pg0; ++pg) {
+                const int first = it.kv_begin + 16 * pg;  // key in slot 0
+                u32x4 seen;
+#pragma unroll
+                for (int jj = 0; jj < 4; ++jj)
+                    seen[jj] = T::pack2(first + 2 * jj < vis_lane ? 1.f : 0.f,
+                                        first + 2 * jj + 1 < vis_lane ? 1.f : 0.f);
+                const int64_t tile = (int64_t)pt[pg0 + pg] * num_kv_heads + it.kv_head;
+                const uint8_t *from = reinterpret_cast<const uint8_t *>(v_pages) + tile * (16 * D) +
+                                      (l & 31) * 16 + 8 * (l >> 5);
+                const int keys = it.kv_end - first - 8 * (l >> 5);
+#pragma unroll
+                for (int blk = 0; blk < NB; ++blk) {
+                    const u32x2 codes = *reinterpret_cast<const u32x2 *>(from + blk * 512);
+                    const uint32_t lo = (nan_codes(codes[0] & codes_in_front(keys)) >> 7) * 0x38u;
+                    const uint32_t hi = (nan_codes(codes[1] & codes_in_front(keys - 4)) >> 7) * 0x38u;
+                    f32x16 n;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) n[v] = 0.f;
+                    n = T::mfma32(as_vec8<T>(decode8<T>(lo, hi, 1.f)), as_vec8<T>(seen), n);
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[blk][v] = n[v] > 0.f ? NAN : o[blk][v];
+                }
+            }
+        }
+    }
 
     // ---- finish: every lane owns one row; the two half-waves hold partial sums ----
     int lane_again = (int)(lane_bytes >> 4);
@@ -431,10 +569,11 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
     }
 }
 
-template <typename T, int D>
-static hipError_t launch_wide_t(const pv_plan *plan, const DeviceLists &dl, const void *q, const void *k_pages,
-                                const void *v_pages, const int32_t *page_table, float scale,
-                                void *out, float *ws_o, float *ws_ml, hipStream_t stream)
+template <typename T, int D, bool KV8>
+static void launch_wide_t(const pv_plan *plan, const DeviceLists &dl, const void *q,
+                          const void *k_pages, const void *v_pages, const uint8_t *k_scales,
+                          const uint8_t *v_scales, const int32_t *page_table, float scale, void *out,
+                          float *ws_o, float *ws_ml, hipStream_t stream)
 {
     const int n = (int)plan->wide.size();
     // A negative scale is applied as |scale| on negated queries, a zero scale as 1 on zeros: so
@@ -444,15 +583,33 @@ static hipError_t launch_wide_t(const pv_plan *plan, const DeviceLists &dl, cons
     const uint32_t q_sign = scale < 0.f ? 0x80008000u : 0u;
     const uint32_t q_keep = c == 0.f ? 0u : 0xFFFFFFFFu;
     if (c == 0.f) c = 1.f;
-    auto kernel = plan->wide_streams ? (plan->wide_renews ? attn_wide_kernel<T, D, true, true>
-                                                          : attn_wide_kernel<T, D, false, true>)
-                                     : (plan->wide_renews ? attn_wide_kernel<T, D, true, false>
-                                                          : attn_wide_kernel<T, D, false, false>);
+    auto kernel = plan->wide_renews ? attn_wide_kernel<T, D, true, false, KV8>
+                                    : attn_wide_kernel<T, D, false, false, KV8>;
+    if constexpr (!KV8) {
+        if (plan->wide_streams)
+            kernel = plan->wide_renews ? attn_wide_kernel<T, D, true, true, false>
+                                       : attn_wide_kernel<T, D, false, true, false>;
+    }
     hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, stream, dl.wide, (const uint16_t *)q,
                        (const uint16_t *)k_pages, (const uint16_t *)v_pages,
                        page_table, plan->max_pages_per_req, plan->num_q_heads,
                        plan->pool.num_kv_heads, plan->group, c, q_keep, q_sign, (uint16_t *)out,
-                       ws_o, ws_ml, plan->num_reqs);
+                       ws_o, ws_ml, plan->num_reqs, k_scales, v_scales);
+}
+
+template <bool KV8>
+static hipError_t launch_wide(const pv_plan *plan, const DeviceLists &dl, const void *q,
+                              const void *k_pages, const void *v_pages, const uint8_t *k_scales,
+                              const uint8_t *v_scales, const int32_t *page_table, float scale,
+                              void *out, float *ws_o, float *ws_ml, hipStream_t stream)
+{
+    if (plan->wide.empty()) return hipSuccess;
+    const bool f = plan->pool.dtype == PV_F16;
+    auto go = plan->pool.head_dim == 128
+                  ? (f ? launch_wide_t<F16, 128, KV8> : launch_wide_t<BF16, 128, KV8>)
+                  : (f ? launch_wide_t<F16, 64, KV8> : launch_wide_t<BF16, 64, KV8>);
+    go(plan, dl, q, k_pages, v_pages, k_scales, v_scales, page_table, scale, out, ws_o, ws_ml,
+       stream);
     return hipGetLastError();
 }
 
@@ -460,17 +617,16 @@ hipError_t launch_attn_wide(const pv_plan *plan, const DeviceLists &dl, const vo
                             const void *v_pages, const int32_t *page_table, float scale, void *out,
                             float *ws_o, float *ws_ml, hipStream_t stream)
 {
-    if (plan->wide.empty()) return hipSuccess;
-    const bool f = plan->pool.dtype == PV_F16;
-    if (plan->pool.head_dim == 128)
-        return f ? launch_wide_t<F16, 128>(plan, dl, q, k_pages, v_pages, page_table, scale, out, ws_o,
-                                           ws_ml, stream)
-                 : launch_wide_t<BF16, 128>(plan, dl, q, k_pages, v_pages, page_table, scale, out,
-                                            ws_o, ws_ml, stream);
-    return f ? launch_wide_t<F16, 64>(plan, dl, q, k_pages, v_pages, page_table, scale, out, ws_o,
-                                      ws_ml, stream)
-             : launch_wide_t<BF16, 64>(plan, dl, q, k_pages, v_pages, page_table, scale, out, ws_o,
-                                       ws_ml, stream);
+    return launch_wide<false>(plan, dl, q, k_pages, v_pages, nullptr, nullptr, page_table, scale, out,
+                              ws_o, ws_ml, stream);
+}
+
+hipError_t launch_attn_kv8_wide(const pv_plan *plan, const DeviceLists &dl, const void *q,
+                                const pv_kv8_pool &pool, const int32_t *page_table, float scale,
+                                void *out, float *ws_o, float *ws_ml, hipStream_t stream)
+{
+    return launch_wide<true>(plan, dl, q, pool.k, pool.v, pool.k_scales, pool.v_scales, page_table,
+                             scale, out, ws_o, ws_ml, stream);
 }
 
 }  // namespace pv

@@ -61,7 +61,6 @@ Tuning default_tuning()
 Tuning kv8_tuning()
 {
     Tuning t = default_tuning();
-    t.wide_min_rows = INT32_MAX;
     t.tile_min_keys = t.tile_batch_min_keys = 0;
     return t;
 }
