@@ -95,6 +95,37 @@ __device__ __forceinline__ int block_exponent(uint32_t mag, int before)
 }
 constexpr int kNoExponent = -1000;
 
+// 16 values divided by the scale, as codes
+template <typename T>
+__device__ __forceinline__ u32x4 encode16(u32x4 a, u32x4 b, float scale)
+{
+    u32x4 codes;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const u32x4 &r = w < 2 ? a : b;
+        const uint32_t lo = Kv8<T>::template encode2<false>(0u, r[2 * (w % 2)], scale);
+        codes[w] = Kv8<T>::template encode2<true>(lo, r[2 * (w % 2) + 1], scale);
+    }
+    return codes;
+}
+
+// The codes of the slots in front of s0 in a K block, rounded anew by the whole wavefront
+template <int D>
+__device__ __forceinline__ void rescale_k(uint8_t *block, int s0, int before, int e)
+{
+    constexpr int LPT = D / 32;
+    const int slot = lane_id() / LPT, c = lane_id() % LPT;
+    if (slot >= s0) return;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        u32x4 *p = reinterpret_cast<u32x4 *>(block + kv8_k_chunk<D>(slot, c + half * LPT));
+        u32x4 codes = *p;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) codes[w] = rescale4(codes[w], before, e);
+        *p = codes;
+    }
+}
+
 template <typename T, int D, int STYLE>
 __device__ __forceinline__ void append_k8(const AppendGroup &g, int h, int num_kv_heads, int64_t tile,
                                           const uint16_t *__restrict__ k_new,
@@ -129,26 +160,11 @@ __device__ __forceinline__ void append_k8(const AppendGroup &g, int h, int num_k
     uint8_t *at = k_pages + tile * (16 * D);
     if (fresh) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            u32x4 codes;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const u32x4 &r = raw[2 * half + w / 2];
-                uint32_t v = Kv8<T>::template encode2<false>(0u, r[2 * (w % 2)], scale);
-                codes[w] = Kv8<T>::template encode2<true>(v, r[2 * (w % 2) + 1], scale);
-            }
-            *reinterpret_cast<u32x4 *>(at + kv8_k_chunk<D>(slot, c + half * LPT)) = codes;
-        }
-    } else if (s0 > 0 && e > before && slot < s0) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            u32x4 *p = reinterpret_cast<u32x4 *>(at + kv8_k_chunk<D>(slot, c + half * LPT));
-            u32x4 codes = *p;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) codes[w] = rescale4(codes[w], before, e);
-            *p = codes;
-        }
+        for (int half = 0; half < 2; ++half)
+            *reinterpret_cast<u32x4 *>(at + kv8_k_chunk<D>(slot, c + half * LPT)) =
+                encode16<T>(raw[2 * half], raw[2 * half + 1], scale);
     }
+    if (s0 > 0 && e > before) rescale_k<D>(at, s0, before, e);
     if (lane == 0 && e != before) scales[tile] = (uint8_t)(e + 127);
 }
 
@@ -188,8 +204,8 @@ __device__ __forceinline__ void append_v8(const AppendGroup &g, int h, int num_k
         codes[0][w] = __builtin_amdgcn_perm(b, a, 0x06040200u);
         codes[1][w] = __builtin_amdgcn_perm(b, a, 0x07050301u);
     }
+    uint8_t *at = v_pages + tile * (16 * D) + d * 16;
     if (lane < D / 2) {
-        uint8_t *at = v_pages + tile * (16 * D) + d * 16;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             u32x4 *p = reinterpret_cast<u32x4 *>(at + 16 * i);
@@ -246,6 +262,133 @@ __global__ __launch_bounds__(128) void kv8_append_kernel(
                                pool.k_scales);
     else
         append_v8<T, D>(g, h, num_kv_heads, tile, v_new, pool.v, pool.v_scales);
+}
+
+// Batches that bring one token a request.  Whole pages a wavefront would leave most lanes without work,
+// so a wavefront of its own takes several heads of one token: the K rows of 128 / (D / 16) heads (lane =
+// head and the 32 dimensions of append_k8), V of a quarter as many (lane = 8 dimensions), or the
+// queries of as many heads as K.  A page that has to be rounded anew is the whole wavefront's work.
+template <typename T, int D, int STYLE>
+__global__ __launch_bounds__(64) void kv8_step_kernel(
+    const AppendGroup *__restrict__ groups, const uint16_t *q_in, uint16_t *q_out /* may be q_in */,
+    const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new,
+    const uint16_t *__restrict__ q_weight, const uint16_t *__restrict__ k_weight, float eps,
+    const float *__restrict__ cos_sin, const int32_t *__restrict__ page_table, int32_t max_pages,
+    int32_t num_q_heads, int32_t num_kv_heads, Kv8Ptrs pool)
+{
+    constexpr int LPT = D / 32, KH = 64 / LPT;  // lanes a head and heads, of K and queries
+    constexpr int VL = D / 8, VH = 64 / VL;     // the same of V
+    const AppendGroup g = groups[blockIdx.x];
+    const int lane = lane_id();
+    const int k_blocks = (num_kv_heads + KH - 1) / KH, v_blocks = (num_kv_heads + VH - 1) / VH;
+    int y = (int)blockIdx.y;
+    if (STYLE >= 0 && y >= k_blocks + v_blocks) {
+        const int h = (y - k_blocks - v_blocks) * KH + lane / LPT, c = lane % LPT;
+        if (h >= num_q_heads) return;
+        const int64_t row = ((int64_t)g.q_row * num_q_heads + h) * D;
+        u32x4 raw[4];
+        load_halves<D>(raw, q_in + row, c);
+        norm_rotate<T, D, STYLE < 0 ? 0 : STYLE>(raw, q_weight, eps, cos_sin + (int64_t)g.t_begin * D,
+                                                 c);
+        uint16_t *to = q_out + row + 16 * c;
+        *reinterpret_cast<u32x4 *>(to) = raw[0];
+        *reinterpret_cast<u32x4 *>(to + 8) = raw[1];
+        *reinterpret_cast<u32x4 *>(to + D / 2) = raw[2];
+        *reinterpret_cast<u32x4 *>(to + D / 2 + 8) = raw[3];
+        return;
+    }
+    const int64_t page = page_table[(int64_t)g.req * max_pages + (g.t_begin >> 4)];
+    const int s0 = g.t_begin & 15;
+    if (y < k_blocks) {
+        const int u = lane / LPT, c = lane % LPT;
+        const bool valid = y * KH + u < num_kv_heads;
+        const int h = valid ? y * KH + u : num_kv_heads - 1;
+        const int64_t tile = page * num_kv_heads + h;
+        u32x4 raw[4];
+        load_halves<D>(raw, k_new + ((int64_t)g.q_row * num_kv_heads + h) * D, c);
+        const int before = s0 > 0 ? (int)pool.k_scales[tile] - 127 : kNoExponent;
+        if constexpr (STYLE >= 0)
+            norm_rotate<T, D, STYLE>(raw, k_weight, eps, cos_sin + (int64_t)g.t_begin * D, c);
+        uint32_t mag = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) mag = max_magnitudes(mag, finite_magnitudes<T>(raw[i][w]));
+#pragma unroll
+        for (int m = 1; m < LPT; m *= 2) mag = max_magnitudes(mag, __shfl_xor(mag, m));
+        const int e = max(needed_exponent<T>(max(mag & 0xFFFFu, mag >> 16)), before);
+        if (__any(e == Kv8<T>::kMaxExp)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    raw[i][w] = e == Kv8<T>::kMaxExp ? limit_to_top<T>(raw[i][w]) : raw[i][w];
+        }
+        if (valid) {
+            uint8_t *at = pool.k + tile * (16 * D);
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                *reinterpret_cast<u32x4 *>(at + kv8_k_chunk<D>(s0, c + half * LPT)) =
+                    encode16<T>(raw[2 * half], raw[2 * half + 1], exp2_scale(e + 127));
+            if (c == 0 && e != before) pool.k_scales[tile] = (uint8_t)(e + 127);
+        }
+        uint64_t grown = s0 > 0 ? __ballot(valid && c == 0 && e > before) : 0;
+        for (; grown; grown &= grown - 1) {
+            const int from = __ffsll((long long)grown) - 1;
+            rescale_k<D>(pool.k + (page * num_kv_heads + y * KH + from / LPT) * (16 * D), s0,
+                         __builtin_amdgcn_readlane(before, from), __builtin_amdgcn_readlane(e, from));
+        }
+        return;
+    }
+    y -= k_blocks;
+    const int u = lane / VL, c = lane % VL;
+    const bool valid = y * VH + u < num_kv_heads;
+    const int h = valid ? y * VH + u : num_kv_heads - 1;
+    const int64_t tile = page * num_kv_heads + h;
+    u32x4 raw = load16(v_new + ((int64_t)g.q_row * num_kv_heads + h) * D + 8 * c);
+    const int before = s0 > 0 ? (int)pool.v_scales[tile] - 127 : kNoExponent;
+    uint32_t mag = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mag = max_magnitudes(mag, finite_magnitudes<T>(raw[w]));
+#pragma unroll
+    for (int m = 1; m < VL; m *= 2) mag = max_magnitudes(mag, __shfl_xor(mag, m));
+    const int e = max(needed_exponent<T>(max(mag & 0xFFFFu, mag >> 16)), before);
+    if (__any(e == Kv8<T>::kMaxExp)) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) raw[w] = e == Kv8<T>::kMaxExp ? limit_to_top<T>(raw[w]) : raw[w];
+    }
+    uint64_t grown = s0 > 0 ? __ballot(valid && c == 0 && e > before) : 0;
+    if (grown) {
+        for (; grown; grown &= grown - 1) {
+            const int from = __ffsll((long long)grown) - 1;
+            const int b = __builtin_amdgcn_readlane(before, from);
+            const int a = __builtin_amdgcn_readlane(e, from);
+            uint8_t *at = pool.v + (page * num_kv_heads + y * VH + from / VL) * (16 * D);
+            for (int d = lane; d < D; d += 64) {
+                u32x4 *p = reinterpret_cast<u32x4 *>(at + d * 16);
+                u32x4 codes = *p;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t front = codes_in_front(s0 - 4 * w);
+                    codes[w] = (rescale4(codes[w], b, a) & front) | (codes[w] & ~front);
+                }
+                *p = codes;
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0);  // the new token's codes, below, lie among these bytes
+        asm volatile("" ::: "memory");
+    }
+    if (valid) {
+        uint8_t *at = pool.v + tile * (16 * D) + c * 128 + s0;
+        const float scale = exp2_scale(e + 127);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t two = Kv8<T>::template encode2<false>(0u, raw[w], scale);
+            at[32 * w] = (uint8_t)two;
+            at[32 * w + 16] = (uint8_t)(two >> 8);
+        }
+        if (c == 0 && e != before) pool.v_scales[tile] = (uint8_t)(e + 127);
+    }
 }
 
 // The inverse: the rows of the plan's new tokens out of the pools, as 16-bit values (exact).
@@ -307,10 +450,14 @@ static void launch_append8_t(const pv_plan *plan, const DeviceLists &dl, const N
                              const void *k_new, const void *v_new, const int32_t *page_table,
                              const Kv8Ptrs &pool, hipStream_t stream)
 {
-    const int q_blocks = STYLE >= 0 && nr.q_in ? (plan->num_q_heads + 1) / 2 : 0;
-    const dim3 grid((unsigned)plan->append_groups.size(),
-                    (unsigned)(plan->pool.num_kv_heads + q_blocks));
-    hipLaunchKernelGGL((kv8_append_kernel<T, D, STYLE>), grid, dim3(128), 0, stream,
+    const int hq = STYLE >= 0 && nr.q_in ? plan->num_q_heads : 0, hkv = plan->pool.num_kv_heads;
+    const bool steps = (int32_t)plan->append_groups.size() == plan->total_q;  // one token a group
+    constexpr int KH = 64 / (D / 32), VH = 64 / (D / 8);
+    const int blocks = steps ? (hkv + KH - 1) / KH + (hkv + VH - 1) / VH + (hq + KH - 1) / KH
+                             : hkv + (hq + 1) / 2;
+    const dim3 grid((unsigned)plan->append_groups.size(), (unsigned)blocks);
+    auto kernel = steps ? kv8_step_kernel<T, D, STYLE> : kv8_append_kernel<T, D, STYLE>;
+    hipLaunchKernelGGL(kernel, grid, dim3(steps ? 64 : 128), 0, stream,
                        dl.append_groups, (const uint16_t *)nr.q_in, (uint16_t *)nr.q_out,
                        (const uint16_t *)k_new, (const uint16_t *)v_new,
                        (const uint16_t *)nr.q_weight, (const uint16_t *)nr.k_weight, nr.eps,
