@@ -67,6 +67,47 @@ def test_a_history_token_by_token(dtype, d):
     assert changes >= 3  # pages whose scale grew with a later token
 
 
+@pytest.mark.parametrize("heads,dtype", [((40, 40, 128), "f16"), ((11, 11, 64), "bf16"),
+                                         ((8, 1, 128), "bf16"), ((35, 35, 64), "f16")])
+@pytest.mark.parametrize("std", [1e-2, 1.0, 50.0])
+def test_one_token_to_every_request(heads, dtype, std):
+    """A batch of generation steps: pages begun, scales kept (1e-2), grown here and there and everywhere."""
+    ctx = [0, 1, 5, 15, 16, 31, 47, 100]
+    b = _batch(ctx, [1] * len(ctx), heads, dtype)
+    before = R.Pools(b)
+    R.append(before, *[R.random_bits((int(b.ctx_lens.sum()), heads[1], heads[2]), dtype, 60 + i)
+                       for i in range(2)], np.zeros_like(b.ctx_lens), b.ctx_lens)
+    k, v = _new_rows(b, 62, std)
+    inf = 0x7C00 if dtype == "f16" else 0x7F80
+    k[2, 0, 3], v[3, 0, 60], k[4, -1] = inf, inf | 1, 0
+    k[6, 0, 9] = v[5, -1, 63] = inf - 1  # the largest finite value
+    _check_append(b, before, k, v)
+
+
+@pytest.mark.parametrize("heads,dtype", [((40, 40, 128), "f16"), ((7, 7, 64), "bf16")])
+def test_batches_of_many_rows(heads, dtype):
+    """More than 64 MiB of rows: the streaming hint, and several heads a wavefront when read back."""
+    new = [2000, 1, 1400, 17] if heads[2] == 128 else [37000, 1, 450, 17]
+    b = _batch([0, 9, 4, 100], new, heads, dtype)
+    assert b.total_q * heads[1] * heads[2] * 4 > 64 << 20
+    k, v = _new_rows(b, 71)
+    run, dev = R.Run(b), R.to_dev(R.Pools(b, "random", seed=2))
+    run.append(dev, k, v)
+    p = R.from_dev(dev, b)
+    for got, new_rows in zip(run.read(dev), (k, v)):
+        # the rows come back within half a step of a code: 2^-4 of the value, or 2^-10 of the block's scale,
+        # which is at most 2^(1 - 448's exponent 8) * its largest value, at most 2^3 here
+        x, y = (H.bits_to_f64(t, dtype) for t in (got, new_rows))
+        assert (np.abs(x - y) <= np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * 2.0 ** -4)).all()
+    for r, lo in ((0, 1984), (2, 4), (3, 100)):  # some pages against the definition
+        n = min(16, int(b.kv_lens[r]) - lo)
+        kk, vv = R.rows(p, r, lo, lo + n)
+        at = int(b.q_start[r]) + lo - int(b.ctx_lens[r])
+        back = run.read(dev)
+        assert np.array_equal(kk, H.bits_to_f64(back[0][at:at + n], dtype))
+        assert np.array_equal(vv, H.bits_to_f64(back[1][at:at + n], dtype))
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_extreme_values(dtype):
     """Zeros, the type's least and largest values, infinities, NaN, and values next to a scale's end."""

@@ -165,15 +165,22 @@ def _same_or_next(got, want, exact):
 @pytest.mark.parametrize("weights", ["both", "none"])
 @pytest.mark.parametrize("heads,dtype", [((6, 3, 128), "bf16"), ((33, 11, 64), "f16"),
                                          ((8, 1, 128), "f16"), ((5, 5, 64), "bf16")])
-def test_into_8_bit_pools_is_norm_rotation_and_append(heads, dtype, weights, style):
+@pytest.mark.parametrize("batch", ["mixed", "steps", "many"])
+def test_into_8_bit_pools_is_norm_rotation_and_append(heads, dtype, weights, style, batch):
     """What the call for 16-bit pools rounds, quantised as the append does: bit for bit in bf16 with norms.
     In f16 the last multiply-add and the rounding to 16 bits may be one instruction, which rounds once
     where two round twice, and without norms the two terms of a rotation may be added in either order.
-    Results differ then only where the exact one lies within an fp32 rounding or two of the middle of
-    two 16-bit values, by one step of them.  So rotated queries may be neighbours, and codes of keys
-    too: the rounding to a code is monotonic, and codes lie at least 16 such steps apart."""
+    In front of the last rounding two results are then at most 2 * 2^-24 * (|a| + |b|) apart, behind
+    it by one 16-bit step (two half steps) more.  Codes of keys are neighbours at the most: they lie at
+    least 2^-9 * 2^e apart, 16 steps where they lie further, and 2^-22 * 448 * 2^e is less."""
     import torch
-    b = _batch(heads, dtype)
+    if batch == "steps":
+        b = _batch(heads, dtype, (0, 1, 15, 40, 31), (1, 1, 1, 1, 1))
+    elif batch == "many":  # over 32 MiB of rows: two heads a wavefront
+        rows = (33 << 20) // (2 * heads[2] * (heads[0] + 2 * heads[1]))
+        b = _batch(heads, dtype, (0, 5), (rows - 60, 61))
+    else:
+        b = _batch(heads, dtype)
     q, k, v, w = _inputs(b)
     exact = dtype == "bf16" and weights == "both"
     if weights == "none":
@@ -194,7 +201,13 @@ def test_into_8_bit_pools_is_norm_rotation_and_append(heads, dtype, weights, sty
         if exact:
             assert np.array_equal(got, q16)
         else:
-            assert (np.abs(got.astype(np.int64) - q16) <= 1).all() and (got != q16).mean() < 5e-3
+            x, y = H.bits_to_f64(got, dtype), H.bits_to_f64(q16, dtype)
+            least = 2.0 ** (-14 if dtype == "f16" else -126)
+            most = np.abs(H.bits_to_f64(q, dtype)).max(axis=2, keepdims=True)
+            if w[0] is not None:  # a normalised row: at most sqrt(D) times the largest weight
+                most = np.sqrt(heads[2]) * np.abs(H.bits_to_f64(w[0], dtype)).max()
+            step = 2 * R.HALF_STEP[dtype] * np.maximum(np.maximum(np.abs(x), np.abs(y)), least)
+            assert (np.abs(x - y) <= step + 2.0 ** -22 * most).all() and (got != q16).mean() < 5e-3
             _close(got, q, w[0], b, style)
     dev = R.to_dev(before)  # keys and values alone
     run.pv.kv8_norm_rope_append_planned(run.plan, None, None, *d[1:], EPS,
