@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "pv_plan.h"
 
@@ -172,6 +173,15 @@ __device__ __forceinline__ void rotate_pair(float a, float b, float c, float s, 
     y = __builtin_fmaf(a, s, b * c);
 }
 
+// The value of a lane M away, by the vector ALU alone (M = 1, 2, 8: lane ^ M; M = 4: a lane of the other
+// four of eight, for values that are the same in four lanes).
+template <int M>
+__device__ __forceinline__ uint32_t other_lane(uint32_t x)
+{
+    constexpr int kCtrl = M == 1 ? 0xB1 : M == 2 ? 0x4E : M == 4 ? 0x141 : 0x128;
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xF, 0xF, true);
+}
+
 // Norm of a row of D elements: 1 / sqrt(mean of the squares + eps).  The squares of 8 elements are
 // added in order, those of chunk i (of 8) and of chunk i + D/16, then neighbours: `pairs` holds such
 // a sum of two chunks for each of the D/16 lanes of a row, or of PER consecutive ones for fewer lanes.
@@ -186,8 +196,15 @@ __device__ __forceinline__ float sum_squares(const float (&x)[8])
 template <int D, int PER = 1>
 __device__ __forceinline__ float norm_factor(float pairs, float eps)
 {
-#pragma unroll
-    for (int m = 1; m < D / 16 / PER; m *= 2) pairs += __shfl_xor(pairs, m);
+    constexpr int LANES = D / 16 / PER;
+    auto add = [&](auto m) {
+        if constexpr (decltype(m)::value < LANES)
+            pairs += __builtin_bit_cast(
+                float, other_lane<decltype(m)::value>(__builtin_bit_cast(uint32_t, pairs)));
+    };
+    add(std::integral_constant<int, 1>{});
+    add(std::integral_constant<int, 2>{});
+    add(std::integral_constant<int, 4>{});
     return 1.f / sqrtf(pairs * (1.f / D) + eps);
 }
 

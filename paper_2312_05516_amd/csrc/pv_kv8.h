@@ -122,6 +122,25 @@ __device__ __forceinline__ uint32_t max_magnitudes(uint32_t a, uint32_t b)
                                                                   __builtin_bit_cast(u2, b)));
 }
 
+// The largest magnitudes (of either half) among LANES neighbouring lanes, in all of them
+template <int LANES>
+__device__ __forceinline__ uint32_t max_of_lanes(uint32_t mag)
+{
+    mag = max_magnitudes(mag, other_lane<1>(mag));
+    if constexpr (LANES > 2) mag = max_magnitudes(mag, other_lane<2>(mag));
+    if constexpr (LANES > 4) mag = max_magnitudes(mag, other_lane<4>(mag));
+    if constexpr (LANES > 8) mag = max_magnitudes(mag, other_lane<8>(mag));
+    if constexpr (LANES > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(mag, mag, false, false);
+        mag = max_magnitudes(r[0], r[1]);
+    }
+    if constexpr (LANES > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(mag, mag, false, false);
+        mag = max_magnitudes(r[0], r[1]);
+    }
+    return mag;
+}
+
 // The least e in the type's range with a <= 448 * 2^e, `magnitude` being the bits of a.
 template <typename T>
 __device__ __forceinline__ int needed_exponent(uint32_t magnitude)

@@ -13,8 +13,6 @@
 // K: lane = (slot, 16 dimensions of either half), whose codes are the pool's 16-byte chunks and
 // which holds both partners of a rotation.  V: lane = two dimensions of all 16 slots, so that the
 // transposition into the pool's runs of 16 slots is byte permutes inside a lane.
-#include <type_traits>
-
 #include "pv_kv8.h"
 
 namespace pv {
@@ -100,8 +98,7 @@ struct Side {
 template <typename T, int D>
 __device__ __forceinline__ int block_exponent(uint32_t mag, int before)
 {
-#pragma unroll
-    for (int m = Side<D>::kLanes / 2; m >= 1; m /= 2) mag = max_magnitudes(mag, __shfl_xor(mag, m));
+    mag = max_of_lanes<Side<D>::kLanes>(mag);
     int most = (int)max(mag & 0xFFFFu, mag >> 16);
     if (D == 128) most = __builtin_amdgcn_readfirstlane(most);
     return max(needed_exponent<T>((uint32_t)most), before);
@@ -384,8 +381,7 @@ __global__ __launch_bounds__(64) void kv8_step_kernel(
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int w = 0; w < 4; ++w) mag = max_magnitudes(mag, finite_magnitudes<T>(raw[i][w]));
-#pragma unroll
-        for (int m = 1; m < LPT; m *= 2) mag = max_magnitudes(mag, __shfl_xor(mag, m));
+        mag = max_of_lanes<LPT>(mag);
         const int e = max(needed_exponent<T>(max(mag & 0xFFFFu, mag >> 16)), before);
         if (__any(e == Kv8<T>::kMaxExp)) {
 #pragma unroll
@@ -420,8 +416,7 @@ __global__ __launch_bounds__(64) void kv8_step_kernel(
     uint32_t mag = 0;
 #pragma unroll
     for (int w = 0; w < 4; ++w) mag = max_magnitudes(mag, finite_magnitudes<T>(raw[w]));
-#pragma unroll
-    for (int m = 1; m < VL; m *= 2) mag = max_magnitudes(mag, __shfl_xor(mag, m));
+    mag = max_of_lanes<VL>(mag);
     const int e = max(needed_exponent<T>(max(mag & 0xFFFFu, mag >> 16)), before);
     if (__any(e == Kv8<T>::kMaxExp)) {
 #pragma unroll

@@ -15,8 +15,6 @@
 // heads first (K rotated + scattered, V scattered as in kv_append_kernel), then the query heads of
 // the group's tokens.  The heads of a token share its angles, which are twice the bytes of one
 // head's row, so a thread loads them once for all its heads, and then all its rows at once.
-#include <type_traits>
-
 #include "pv_device.h"
 
 namespace pv {
@@ -45,6 +43,13 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
     const uint16_t *src = (is_q ? q_in : k_new) + src_off;
 
     const uint16_t *weight = NORM ? (is_q ? q_weight : k_weight) : nullptr;
+    // a lane's weights: of chunk c8 and, for pairs across the halves of a head, of its partner
+    u32x4 weights[2];
+    if (NORM && weight) {
+        const int c8 = STYLE == 0 ? t % CH : t % (CH / 2);
+        weights[0] = load16(weight + 8 * c8);
+        if constexpr (STYLE == 1) weights[1] = load16(weight + D / 2 + 8 * c8);
+    }
 
     int64_t tile = 0;
     int slot0 = 0;
@@ -79,9 +84,15 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
                 unpack8<T>(raw[i], x);
                 if (NORM && weight) {
                     float w[8];
-                    unpack8<T>(load16(weight + 8 * c8), w);
+                    unpack8<T>(weights[0], w);
                     const float mine = sum_squares(x);
-                    const float r = norm_factor<D>(mine + __shfl_xor(mine, CH / 2), eps);
+                    float partner;  // the chunk half a row away
+                    if constexpr (D == 128)
+                        partner = __builtin_bit_cast(
+                            float, other_lane<8>(__builtin_bit_cast(uint32_t, mine)));
+                    else
+                        partner = __shfl_xor(mine, 4);
+                    const float r = norm_factor<D>(mine + partner, eps);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = x[e] * r * w[e];
                 }
@@ -128,8 +139,8 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
                 unpack8<T>(rb[m], xb);
                 if (NORM && weight) {
                     float wa[8], wb[8];
-                    unpack8<T>(load16(weight + 8 * c8), wa);
-                    unpack8<T>(load16(weight + D / 2 + 8 * c8), wb);
+                    unpack8<T>(weights[0], wa);
+                    unpack8<T>(weights[1], wb);
                     const float r =
                         norm_factor<D>(sum_squares(xa) + sum_squares(xb), eps);
 #pragma unroll
