@@ -39,20 +39,29 @@
 // anyway before the second product; the launch uses it only while |scale*log2(e)| <= 0.25 (1/sqrt(D)
 // for D >= 34), and the exact fp32 scaling otherwise and for plans with few items of this kernel
 // (pv_plan::tile_scales_scores).
+//
+// KV8: the pools hold 8-bit codes (pv_kv8.h).  In place of the copies every thread reads 16 codes of K
+// and 16 of V of a block, five blocks ahead, into one of two register sets, and two iterations later,
+// in the slots of the value product, widens them to 16 bits and stores them in LDS where a copy would
+// have put them (four stages of it suffice: block b + 3 is written while b to b + 2 are read).  So a
+// code is widened once for 256 rows, 16 conversions and 4 stores for a thread's 32 matrix-core
+// instructions.  Scores are always scaled in fp32.
 #include <type_traits>
 
-#include "pv_device.h"
+#include "pv_kv8.h"
 
 namespace pv {
 
-template <typename T, bool PRE>
+template <typename T, bool PRE, bool KV8>
 __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     const WorkItem *__restrict__ items, const uint16_t *__restrict__ q,
     const uint16_t *__restrict__ k_pages, const uint16_t *__restrict__ v_pages,
     const int32_t *__restrict__ page_table, int32_t max_pages, int32_t num_q_heads,
     int32_t num_kv_heads, int32_t group, float scale_log2e, uint32_t q_sign,
-    uint16_t *__restrict__ out, float *__restrict__ ws_o, float *__restrict__ ws_ml)
+    uint16_t *__restrict__ out, float *__restrict__ ws_o, float *__restrict__ ws_ml,
+    const uint8_t *__restrict__ k_scales, const uint8_t *__restrict__ v_scales)
 {
+    static_assert(!(PRE && KV8), "no such instance");
     constexpr int D = 128;
     constexpr int SUB = 2;                      // 32-row sub-tiles per wavefront
     constexpr int BK = 32;                      // keys per block
@@ -61,7 +70,7 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     constexpr int TILE_BYTES = 16 * D * 2;      // one (page, head) tile
     constexpr int HALF_BYTES = 2 * TILE_BYTES;  // K (or V) part of a stage: two pages
     constexpr int STAGE_BYTES = 2 * HALF_BYTES;
-    constexpr int STAGES = 8;
+    constexpr int STAGES = KV8 ? 4 : 8;
     constexpr int PF = 6;                       // blocks the copies run ahead of their use
     constexpr int LOADS = STAGE_BYTES / 1024 / 4;  // 1 KiB copies per wavefront per block
     static_assert(LOADS == 4, "piece layout below assumes four pieces per wavefront");
@@ -69,7 +78,10 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     // the item's page ids, two per block: read back through LDS, whose results return in order
     // with the operand reads (a scalar load in the loop would make every wait for an operand a
     // wait for that load too)
-    __shared__ __attribute__((aligned(8))) int32_t page_lds[kTileMaxPages];
+    __shared__ __attribute__((aligned(8))) int32_t page_lds[KV8 ? 2 : kTileMaxPages];
+    // KV8: page id, and the bytes of its K and V scales (K in the low one)
+    __shared__ u32x2 page8_lds[KV8 ? kTileMaxPages : 1];
+    __shared__ int left_out;  // KV8: whether a NaN was left out of a masked block
 
     const WorkItem it = items[blockIdx.x];
     const int lane = lane_id();
@@ -131,8 +143,16 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     const uint32_t lane_bytes = (uint32_t)lane * 16u;
 
     // page ids of a block (two pages; a page past the end is never used, so any valid id will do)
-    for (int i = (int)threadIdx.x; i < 2 * nblocks && i < kTileMaxPages; i += 256)
-        page_lds[i] = pt[pg0 + i <= last_pg ? pg0 + i : last_pg];
+    for (int i = (int)threadIdx.x; i < 2 * nblocks && i < kTileMaxPages; i += 256) {
+        const int32_t id = pt[pg0 + i <= last_pg ? pg0 + i : last_pg];
+        if constexpr (KV8) {
+            const int64_t tile = (int64_t)id * num_kv_heads + it.kv_head;
+            page8_lds[i] = u32x2{(uint32_t)id, k_scales[tile] | (uint32_t)v_scales[tile] << 8};
+        } else {
+            page_lds[i] = id;
+        }
+    }
+    if (KV8 && threadIdx.x == 0) left_out = 0;
     __syncthreads();
     // in two steps, so that the pipelined loop can put other work between the LDS read and the
     // first use of its result
@@ -161,6 +181,61 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     auto dma_block = [&](int b, int id0, int id1) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) dma_piece(b, id0, id1, i);
+    };
+
+    // KV8.  Wavefront w reads from page w / 2 of a block: chunk at / 16 of slot at % 16 of K, the 16 slots
+    // of dimension `at` of V, at = thread within the page.  Block b is in register set b % 2.
+    const int in_page = (int)threadIdx.x & 127;
+    const uint32_t k8_off = (uint32_t)kv8_k_chunk<D>(in_page & 15, in_page >> 4);
+    const uint32_t v8_off = (uint32_t)in_page * 16;
+    const int k8_lds = (w >> 1) * TILE_BYTES + ((in_page >> 4) * 32 + (in_page & 15)) * 16;
+    const int v8_lds = HALF_BYTES + (w >> 1) * TILE_BYTES + in_page * 16;
+    const uint32_t page8_bytes = (uint32_t)num_kv_heads * (16 * D);
+    const uint8_t *k8_src =
+        reinterpret_cast<const uint8_t *>(k_pages) + (uint64_t)it.kv_head * (16 * D);
+    const uint8_t *v8_src =
+        reinterpret_cast<const uint8_t *>(v_pages) + (uint64_t)it.kv_head * (16 * D);
+    u32x4 k8[2], v8[2];
+    float ks8[2], vs8[2];  // their scales
+    auto page8_request = [&](int b) {
+        const int bb = b < nblocks ? b : nblocks - 1;
+        return page8_lds[2 * bb + (w >> 1)];
+    };
+    // the page that is read next: its offset in the pools, and its scales
+    uint64_t page8_off = 0;
+    uint32_t page8_scales = 0;
+    auto page8_take = [&](u32x2 entry) {
+        page8_off = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)entry[0]) * page8_bytes;
+        page8_scales = (uint32_t)__builtin_amdgcn_readfirstlane((int)entry[1]);
+    };
+    auto load8 = [&](int set) {
+        k8[set] = load16(k8_src + page8_off + k8_off);
+        v8[set] = load16(v8_src + page8_off + v8_off);
+        ks8[set] = exp2_scale((int)(page8_scales & 0xFFu));
+        vs8[set] = exp2_scale((int)(page8_scales >> 8));
+    };
+    // below it nothing is masked for any row of the item
+    const int item_unmasked = min(it.ctx + it.row_begin / group + 1, it.kv_end);
+    // block b, in register set `set`, to its stage (outside the hand-laid schedule)
+    auto widen8 = [&](int b, int set) {
+        if (it.kv_begin + BK * (b + 1) > item_unmasked) {
+            // A NaN among values that some row does not see: zero times it would be NaN in that row too.
+            // It is left out, and given to the rows that see it at the end.
+            uint32_t any = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t nan = nan_codes(v8[set][i]);
+                any |= nan;
+                v8[set][i] &= ~((nan >> 7) * 0xFFu);
+            }
+            if (any) left_out = 1;
+        }
+        unsigned char *stage = smem[b % STAGES];
+        *reinterpret_cast<u32x4 *>(stage + k8_lds) = decode8<T>(k8[set][0], k8[set][1], ks8[set]);
+        *reinterpret_cast<u32x4 *>(stage + k8_lds + 256) = decode8<T>(k8[set][2], k8[set][3], ks8[set]);
+        *reinterpret_cast<u32x4 *>(stage + v8_lds) = decode8<T>(v8[set][0], v8[set][1], vs8[set]);
+        *reinterpret_cast<u32x4 *>(stage + v8_lds + D * 16) =
+            decode8<T>(v8[set][2], v8[set][3], vs8[set]);
     };
 
     f32x16 o[SUB][NB];
@@ -303,7 +378,9 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     auto publish = [&](bool more) {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
-        if (more)
+        if constexpr (KV8)  // the stores of block b + 3 to LDS; loads may stay in flight
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        else if (more)
             __builtin_amdgcn_s_waitcnt(waitcnt_imm((PF - 3) * LOADS, 15));
         else
             __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 15));
@@ -312,12 +389,23 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     };
 
     // ---- prologue: copies of blocks 0..PF-1 on their way, blocks 0..2 landed and published ----
-    int id0, id1;
-    for (int b = 0; b < PF && b < nblocks; ++b) {
-        page_ids(b, id0, id1);
-        dma_block(b, id0, id1);
+    int id0 = 0, id1 = 0;
+    if constexpr (KV8) {
+        // blocks 0 to 2 written (a block past the end is the last one again), 3 and 4 on their way
+#pragma unroll
+        for (int b = 0; b < 5; ++b) {
+            if (b >= 2) widen8(b - 2, b % 2);
+            page8_take(page8_request(b));
+            load8(b % 2);
+        }
+        page8_take(page8_request(5));
+    } else {
+        for (int b = 0; b < PF && b < nblocks; ++b) {
+            page_ids(b, id0, id1);
+            dma_block(b, id0, id1);
+        }
+        page_ids(PF, id0, id1);
     }
-    page_ids(PF, id0, id1);
     publish(nblocks > PF);
 
     f32x16 s[SUB], sn[SUB];
@@ -345,7 +433,11 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     //   then the test for a reference update, and the barrier.
     f32x16 cinit[SUB];
     float thr_rel[SUB];  // PRE: threshold for block maxima that are relative to the reference
-    auto fast_step = [&](int b, const f32x16 (&cur)[SUB], f32x16 (&nxt)[SUB]) {
+    // KV8, in place of the copies and the page ids: in slots 16-23 two conversions each of block b+3
+    // (loaded two iterations ago), stored two slots behind, the load of block b+5 in slot 25, the
+    // entry of the page after it requested in slot 21 and taken in slot 31.
+    auto fast_step = [&](int b, const f32x16 (&cur)[SUB], f32x16 (&nxt)[SUB], auto parity) {
+        constexpr int SET = (decltype(parity)::value + 3) % 2;  // of blocks b+3 and b+5
         const unsigned char *sb = smem[b % STAGES];
         const unsigned char *sk1 = smem[(b + 1) % STAGES];
         const unsigned char *sk = smem[(b + 2) % STAGES];
@@ -359,7 +451,11 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
         u32x2 next_ids;
         // how many of the 32 row-sum additions each of the slots 16-31 takes: as many as fit
         // beside what the slot already carries
-        constexpr int kSumAdds[16] = {0, 3, 1, 3, 0, 0, 2, 3, 2, 3, 2, 3, 3, 3, 1, 3};
+        constexpr int kSumAdds[16] = {KV8 ? 1 : 0, KV8 ? 1 : 3, 1, KV8 ? 1 : 3, KV8 ? 1 : 0,
+                                      KV8 ? 1 : 0, KV8 ? 1 : 2, KV8 ? 1 : 3, KV8 ? 3 : 2, 3,
+                                      KV8 ? 3 : 2, 3,           3,           3,
+                                      KV8 ? 3 : 1, 3};
+        u32x4 wide8[4];
 #pragma unroll
         for (int slot = 0; slot < 32; ++slot) {
             // --- the slot's matrix-core instruction
@@ -431,6 +527,25 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
             // (the scalar address arithmetic of a piece goes one slot ahead of its copy, into
             // slots that have no operand read, so that no slot carries more than about five
             // instructions next to its matrix-core instruction)
+            if constexpr (KV8) {
+                if (slot >= 16 && slot < 24) {
+                    const int word = (slot - 16) % 4;  // of K, then of V
+                    const uint32_t codes = slot < 20 ? k8[SET][word] : v8[SET][word];
+                    const float scale = slot < 20 ? ks8[SET] : vs8[SET];
+                    u32x4 &to = wide8[(slot - 16) / 2];
+                    to[2 * (word % 2)] = Kv8<T>::template decode2<false>(codes, scale);
+                    to[2 * (word % 2) + 1] = Kv8<T>::template decode2<true>(codes, scale);
+                }
+                if (slot >= 18 && slot <= 24 && slot % 2 == 0) {
+                    const int i = (slot - 18) / 2;
+                    unsigned char *stage = smem[(b + 3) % STAGES];
+                    *reinterpret_cast<u32x4 *>(stage + (i < 2 ? k8_lds + 256 * i
+                                                              : v8_lds + D * 16 * (i - 2))) = wide8[i];
+                }
+                if (slot == 21) next_ids = page8_request(b + 6);
+                if (slot == 25) load8(SET);
+                if (slot == 31) page8_take(next_ids);
+            } else {
             if (slot == 16) {
                 dma_off[0] = (uint64_t)(uint32_t)id0 * page_bytes;
                 dma_off[1] = (uint64_t)(uint32_t)id1 * page_bytes;
@@ -445,6 +560,7 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
             }
             if (slot == 21) next_ids = page_ids_request(b + PF + 1);
             if (slot == 31) page_ids_take(next_ids, id0, id1);
+            }
             // --- maximum of block b+1's results, two registers per slot and sub-tile
             if (slot >= 20 && slot < 28) {
                 const int i = slot - 20;
@@ -466,7 +582,8 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        lds_dma16(dma_src[3], lane_bytes, smem[(b + PF) % STAGES] + (w + 4 * 3) * 1024);
+        if constexpr (!KV8)
+            lds_dma16(dma_src[3], lane_bytes, smem[(b + PF) % STAGES] + (w + 4 * 3) * 1024);
 #pragma unroll
         for (int u = 0; u < SUB; ++u) l_run[u] += psum[u];
         if constexpr (PRE) {
@@ -500,6 +617,11 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     // pipelined iteration has no further block to copy: it fetches the last block once more, into
     // a stage nobody reads again, so that the count of copies in flight stays what the waits assume
     int nfast = (unmasked_end - it.kv_begin) / BK - 1;
+    if constexpr (KV8) {
+        // nor does the pipelined loop widen blocks that are masked for some row of the item (see widen8)
+        const int widened = (item_unmasked - it.kv_begin) / BK - 3;
+        if (item_unmasked < it.kv_end && nfast > widened) nfast = widened;
+    }
     if (nfast < 0) nfast = 0;
     nfast &= ~1;  // pairs: the results ping-pong between two register sets without copies
 
@@ -520,8 +642,8 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
             asm volatile("s_nop 1" ::: "memory");  // cinit feeds a pinned instruction next
         }
         for (; b < nfast; b += 2) {
-            fast_step(b, s, sn);
-            fast_step(b + 1, sn, s);
+            fast_step(b, s, sn, std::integral_constant<int, 0>{});
+            fast_step(b + 1, sn, s, std::integral_constant<int, 1>{});
         }
         if constexpr (PRE) {  // back to scores for the masked loop
 #pragma unroll
@@ -534,8 +656,19 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     // ---- masked loop: blocks at the causal boundary / the end of the sequence ----
     for (; b < nblocks; ++b) {
         const bool more = b + PF < nblocks;
-        if (more) dma_block(b + PF, id0, id1);
-        page_ids(b + PF + 1, id0, id1);
+        if constexpr (KV8) {
+            if (b & 1) {
+                widen8(b + 3, 0);
+                load8(0);
+            } else {
+                widen8(b + 3, 1);
+                load8(1);
+            }
+            page8_take(page8_request(b + 6));
+        } else {
+            if (more) dma_block(b + PF, id0, id1);
+            page_ids(b + PF + 1, id0, id1);
+        }
         const int kb0 = it.kv_begin + BK * b;
         if (kb0 < wave_end) softmax_pv(s, smem[b % STAGES], kb0, std::true_type{});
         if (b + 1 < nblocks && kb0 + BK < wave_end) {
@@ -544,6 +677,42 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
         }
         read_k(b + 2);
         publish(more);
+    }
+
+    if constexpr (KV8) {
+        // NaNs that were left out: counted for each row and dimension by one more product, of ones in
+        // their places with ones for the keys that a row sees
+        if (left_out) {
+#pragma unroll 1
+            for (int pg = max(item_unmasked - it.kv_begin, 0) / BK * 2; pg <= last_pg - pg0; ++pg) {
+                const int first = it.kv_begin + 16 * pg + 8 * h;  // key of the lane's first slot
+                const int64_t tile = (int64_t)page8_lds[pg][0] * num_kv_heads + it.kv_head;
+                const uint8_t *from = reinterpret_cast<const uint8_t *>(v_pages) + tile * (16 * D) +
+                                      q32 * 16 + 8 * h;
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    const int end = min(vis_end[u], it.kv_end);
+                    u32x4 seen;
+#pragma unroll
+                    for (int jj = 0; jj < 4; ++jj)
+                        seen[jj] = T::pack2(first + 2 * jj < end ? 1.f : 0.f,
+                                            first + 2 * jj + 1 < end ? 1.f : 0.f);
+#pragma unroll
+                    for (int blk = 0; blk < NB; ++blk) {
+                        const u32x2 codes = *reinterpret_cast<const u32x2 *>(from + blk * 512);
+                        const int keys = it.kv_end - first;
+                        const uint32_t lo = (nan_codes(codes[0] & codes_in_front(keys)) >> 7) * 0x38u;
+                        const uint32_t hi = (nan_codes(codes[1] & codes_in_front(keys - 4)) >> 7) * 0x38u;
+                        f32x16 n;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) n[v] = 0.f;
+                        n = T::mfma32(as_vec8<T>(decode8<T>(lo, hi, 1.f)), as_vec8<T>(seen), n);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) o[u][blk][v] = n[v] > 0.f ? NAN : o[u][blk][v];
+                    }
+                }
+            }
+        }
     }
 
     // ---- finish: every lane owns one row per sub-tile; the two half-waves hold partial sums ----
@@ -583,36 +752,35 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
     }
 }
 
-template <typename T>
-static hipError_t launch_tile256_t(const pv_plan *plan, const DeviceLists &dl, const void *q, const void *k_pages,
-                                   const void *v_pages, const int32_t *page_table, float scale,
-                                   void *out, float *ws_o, float *ws_ml, hipStream_t stream)
+template <typename T, bool KV8>
+static void launch_tile256_t(const pv_plan *plan, const DeviceLists &dl, const void *q,
+                             const void *k_pages, const void *v_pages, const uint8_t *k_scales,
+                             const uint8_t *v_scales, const int32_t *page_table, float scale,
+                             void *out, float *ws_o, float *ws_ml, hipStream_t stream)
 {
     const int n = (int)plan->tile256.size();
     const float c_signed = scale * kLog2e;
     const float c_abs = c_signed < 0.f ? -c_signed : c_signed;
-    // (a zero scale in fp32 would make NaN of a masked score, minus infinity)
-    if (c_abs <= 0.25f && (!plan->tile_scales_scores || c_abs == 0.f)) {
-        // queries pre-multiplied by scale*log2(e): the sign travels with them
-        hipLaunchKernelGGL((attn_tile256_kernel<T, true>), dim3(n), dim3(256), 0, stream,
-                           dl.tile256, (const uint16_t *)q, (const uint16_t *)k_pages,
-                           (const uint16_t *)v_pages, page_table, plan->max_pages_per_req,
-                           plan->num_q_heads, plan->pool.num_kv_heads, plan->group, c_signed, 0u,
-                           (uint16_t *)out, ws_o, ws_ml);
-    } else {
-        const uint32_t q_sign = scale < 0.f ? 0x80008000u : 0u;
-        hipLaunchKernelGGL((attn_tile256_kernel<T, false>), dim3(n), dim3(256), 0, stream,
-                           dl.tile256, (const uint16_t *)q, (const uint16_t *)k_pages,
-                           (const uint16_t *)v_pages, page_table, plan->max_pages_per_req,
-                           plan->num_q_heads, plan->pool.num_kv_heads, plan->group, c_abs, q_sign,
-                           (uint16_t *)out, ws_o, ws_ml);
+    auto go = [&](auto kernel, float c, uint32_t q_sign) {
+        hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, stream, dl.tile256, (const uint16_t *)q,
+                           (const uint16_t *)k_pages, (const uint16_t *)v_pages, page_table,
+                           plan->max_pages_per_req, plan->num_q_heads, plan->pool.num_kv_heads,
+                           plan->group, c, q_sign, (uint16_t *)out, ws_o, ws_ml, k_scales, v_scales);
+    };
+    if constexpr (!KV8) {
+        // (a zero scale in fp32 would make NaN of a masked score, minus infinity)
+        if (c_abs <= 0.25f && (!plan->tile_scales_scores || c_abs == 0.f))
+            // queries pre-multiplied by scale*log2(e): the sign travels with them
+            return go(attn_tile256_kernel<T, true, false>, c_signed, 0u);
     }
-    return hipGetLastError();
+    go(attn_tile256_kernel<T, false, KV8>, c_abs, scale < 0.f ? 0x80008000u : 0u);
 }
 
-hipError_t launch_attn_tile256(const pv_plan *plan, const DeviceLists &dl, const void *q, const void *k_pages,
-                               const void *v_pages, const int32_t *page_table, float scale,
-                               void *out, float *ws_o, float *ws_ml, hipStream_t stream)
+template <bool KV8>
+static hipError_t launch_tile256(const pv_plan *plan, const DeviceLists &dl, const void *q,
+                                 const void *k_pages, const void *v_pages, const uint8_t *k_scales,
+                                 const uint8_t *v_scales, const int32_t *page_table, float scale,
+                                 void *out, float *ws_o, float *ws_ml, hipStream_t stream)
 {
     if (plan->tile256.empty()) return hipSuccess;
     if (plan->pool.head_dim != 128) return hipErrorInvalidValue;  // the plan never does this
@@ -620,11 +788,25 @@ hipError_t launch_attn_tile256(const pv_plan *plan, const DeviceLists &dl, const
         if (w.row_count != kTileRows || w.kv_end <= w.kv_begin || w.kv_begin % kKvBlock != 0 ||
             (int64_t)w.kv_end - w.kv_begin > (int64_t)kTileMaxPages * 16)
             return hipErrorInvalidValue;
-    return plan->pool.dtype == PV_F16
-               ? launch_tile256_t<F16>(plan, dl, q, k_pages, v_pages, page_table, scale, out, ws_o,
-                                       ws_ml, stream)
-               : launch_tile256_t<BF16>(plan, dl, q, k_pages, v_pages, page_table, scale, out, ws_o,
-                                        ws_ml, stream);
+    auto go = plan->pool.dtype == PV_F16 ? launch_tile256_t<F16, KV8> : launch_tile256_t<BF16, KV8>;
+    go(plan, dl, q, k_pages, v_pages, k_scales, v_scales, page_table, scale, out, ws_o, ws_ml, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_attn_tile256(const pv_plan *plan, const DeviceLists &dl, const void *q, const void *k_pages,
+                               const void *v_pages, const int32_t *page_table, float scale,
+                               void *out, float *ws_o, float *ws_ml, hipStream_t stream)
+{
+    return launch_tile256<false>(plan, dl, q, k_pages, v_pages, nullptr, nullptr, page_table, scale,
+                                 out, ws_o, ws_ml, stream);
+}
+
+hipError_t launch_attn_kv8_tile256(const pv_plan *plan, const DeviceLists &dl, const void *q,
+                                   const pv_kv8_pool &pool, const int32_t *page_table, float scale,
+                                   void *out, float *ws_o, float *ws_ml, hipStream_t stream)
+{
+    return launch_tile256<true>(plan, dl, q, pool.k, pool.v, pool.k_scales, pool.v_scales, page_table,
+                                scale, out, ws_o, ws_ml, stream);
 }
 
 }  // namespace pv

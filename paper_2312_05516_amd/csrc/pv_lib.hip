@@ -41,6 +41,9 @@ hipError_t launch_kv8_append(const pv_plan *plan, const DeviceLists &dl, const N
 hipError_t launch_kv8_read(const pv_plan *plan, const DeviceLists &dl, const pv_kv8_pool &pool,
                            const int32_t *page_table, void *k_rows, void *v_rows,
                            hipStream_t stream);
+hipError_t launch_attn_kv8_tile256(const pv_plan *plan, const DeviceLists &dl, const void *q,
+                                   const pv_kv8_pool &pool, const int32_t *page_table, float scale,
+                                   void *out, float *ws_o, float *ws_ml, hipStream_t stream);
 hipError_t launch_attn_kv8_wide(const pv_plan *plan, const DeviceLists &dl, const void *q,
                                 const pv_kv8_pool &pool, const int32_t *page_table, float scale,
                                 void *out, float *ws_o, float *ws_ml, hipStream_t stream);
@@ -442,6 +445,12 @@ pv_status pv_kv8_multi_token_paged_attn_planned(pv_plan *plan, const void *q,
     s = pv::ensure_ready(plan, true);
     if (s != PV_OK) return s;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    {
+        pv::KernelTimer t(plan, 4, st, !plan->tile256.empty());
+        if (pv::launch_attn_kv8_tile256(plan, plan->dev, q, *pool, page_table, scale, out, ws_o, ws_ml,
+                                        st) != hipSuccess)
+            return PV_ERR_HIP;
+    }
     {
         pv::KernelTimer t(plan, 1, st, !plan->wide.empty());
         if (pv::launch_attn_kv8_wide(plan, plan->dev, q, *pool, page_table, scale, out, ws_o, ws_ml,

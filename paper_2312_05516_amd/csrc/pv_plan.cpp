@@ -58,13 +58,6 @@ Tuning default_tuning()
     return t;
 }
 
-Tuning kv8_tuning()
-{
-    Tuning t = default_tuning();
-    t.tile_min_keys = t.tile_batch_min_keys = 0;
-    return t;
-}
-
 // Whether the full 256-row tiles of a (request, KV head) unit go to the 256-row kernel: that
 // kernel exists for head size 128 and pays off when an item streams many 32-key blocks.
 static bool use_tile256(const pv_pool_desc *pool, const Tuning &tune, int64_t rows_total,
@@ -868,7 +861,7 @@ pv_status pv_plan_create_kv8(const pv_pool_desc *pool, int32_t num_q_heads,
                              int32_t max_pages_per_req, pv_plan **plan)
 {
     return pv::build_plan(pool, num_q_heads, ctx_lens, q_lens, num_reqs, max_pages_per_req,
-                          pv::kv8_tuning(), plan, true);
+                          pv::default_tuning(), plan, true);
 }
 
 int32_t pv_plan_is_kv8(const pv_plan *plan) { return plan ? (plan->kv8 ? 1 : 0) : -1; }

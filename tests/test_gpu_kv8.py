@@ -224,6 +224,23 @@ def test_narrow_lists_in_two_terms():
     assert np.linalg.norm(got - want) / np.linalg.norm(want) < 1.8e-3  # a result's own rounding: 1.66e-3
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("ctx,new,heads", [
+    ([900, 70, 300], [70, 128, 33], (8, 2, 128)),    # tiles that end at every place of a block, rests
+    ([0, 1, 31], [256, 300, 64], (4, 1, 128)),       # first prompts
+    ([4097, 15], [256, 257], (2, 2, 128)),
+    ([5000, 9000], [64, 1], (8, 1, 128)),            # cut into parts, and a generation step beside
+])
+def test_long_prompts_in_tiles_of_256_rows(monkeypatch, ctx, new, heads, dtype):
+    monkeypatch.setenv("PV_TILE_MIN_KEYS", "64")
+    b = _batch(ctx, new, heads, dtype)
+    run = R.Run(b)
+    assert run.pv.plan_num_work_items(run.plan, 3) > 0
+    p, q = R.filled(b, 135)
+    for scale in (b.scale, 0.0, -1.2):
+        _check_attention(b, p, q, scale=scale)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.07, 1.5])
 @pytest.mark.parametrize("heads,dtype", [((8, 1, 128), "bf16"), ((3, 3, 64), "f16")])
 def test_scales(scale, heads, dtype):
@@ -246,10 +263,13 @@ def test_scores_of_any_size_and_blocks_of_any_scale():
     _check_attention(b, p, R.random_bits((b.total_q, 4, 128), "bf16", 162))
 
 
-def test_nan_and_infinity_stay_in_their_rows():
+@pytest.mark.parametrize("group,tiles,d", [(1, "0", 128), (1, "0", 64), (4, "0", 128), (16, "0", 64),
+                                           (16, "64", 128)])
+def test_nan_and_infinity_stay_in_their_rows(monkeypatch, group, tiles, d):
     """A NaN among cached values reaches the rows that see it, and no others; one behind the end of a
-    sequence reaches nobody (every unused slot of `filled` is NaN)."""
-    b = _batch([40, 40], [30, 1], (2, 2, 128), "f16")
+    sequence reaches nobody (every unused slot of `filled` is NaN).  In all three kernels."""
+    monkeypatch.setenv("PV_TILE_MIN_KEYS", tiles)
+    b = _batch([40, 40], [30, 1], (2 * group, 2, d), "f16")
     p, q = R.filled(b, 170)
     page = int(b.page_table[0, 3])  # positions 48..63 of the first request; its rows see 40 + i
     codes = p.slots("v", page, 1)
@@ -257,9 +277,15 @@ def test_nan_and_infinity_stay_in_their_rows():
     p.put("v", page, 1, codes)
     got = R.Run(b).attend(R.to_dev(p), q)
     nan = np.isnan(got)
-    assert nan[10:30, 1, 17].all()
-    nan[10:30, 1, 17] = False
+    assert nan[10:30, group:, 17].all()
+    nan[10:30, group:, 17] = False
     assert not nan.any()
+    k = p.slots("k", page, 0)  # and one among the keys, of the other head: the whole rows that see it
+    k[9, 5] = 0xFF
+    p.put("k", page, 0, k)
+    got = R.Run(b).attend(R.to_dev(p), q)
+    assert np.isnan(got[17:30, :group]).all() and not np.isnan(got[:17, :group]).any()
+    assert not np.isnan(got[30]).any()
 
 
 @pytest.mark.parametrize("new", [1, 40])

@@ -65,9 +65,10 @@ def test_plans_for_8_bit_pools():
     assert pv.plan_is_kv8(p) and not pv.plan_is_kv8(_plan(pv.plan_create))
     assert pv._lib.pv_plan_is_kv8(None) == -1
     assert pv.plan_total_q(p) == 4
-    # long prompts: no items of the 256-row kernel
-    q = _plan(ctx=(20000, 9000), new=(700, 512), heads=(64, 8, 128), max_pages=2000, pages=4000)
-    assert pv.plan_num_work_items(q, 3) == 0
+    # the same kernels as for 16-bit pools: long prompts, prompts, generation steps
+    for ctx, new, kind in (((20000,) * 8, (512,) * 8, 3), ((900, 300), (100, 90), 1), ((900, 300), (1, 1), 0)):
+        q = _plan(ctx=ctx, new=new, heads=(64, 8, 128), max_pages=2000, pages=20000)
+        assert [pv.plan_num_work_items(q, k) > 0 for k in (0, 1, 3)] == [kind == k for k in (0, 1, 3)]
     for bad, status in (((pv.pool_desc(4, 2, 96, "f16"), 4, [1], [1], 4), UNSUPPORTED),
                         ((pv.pool_desc(4, 2, 64, "f16"), 3, [1], [1], 4), INVALID),
                         ((pv.pool_desc(4, 2, 64, "f16"), 4, [-1], [1], 4), INVALID),
