@@ -173,6 +173,10 @@ _lib.pv_kv8_multi_token_paged_attn_planned.argtypes = [_vp, _vp, _kv8p, _vp, cty
 # ------------------------------------------------------------------ marshalling helpers
 def _ptr(x) -> Optional[int]:
     """Device (or host) address of a torch tensor / numpy array / int / None."""
+    if type(x) is torch.Tensor:  # nearly always, and a call has up to nine of them
+        if x.is_contiguous():
+            return x.data_ptr()
+        raise ValueError("tensor arguments must be contiguous")
     if x is None:
         return None
     if isinstance(x, int):

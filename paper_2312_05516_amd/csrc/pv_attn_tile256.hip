@@ -451,10 +451,9 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
         u32x2 next_ids;
         // how many of the 32 row-sum additions each of the slots 16-31 takes: as many as fit
         // beside what the slot already carries
-        constexpr int kSumAdds[16] = {KV8 ? 1 : 0, KV8 ? 1 : 3, 1, KV8 ? 1 : 3, KV8 ? 1 : 0,
-                                      KV8 ? 1 : 0, KV8 ? 1 : 2, KV8 ? 1 : 3, KV8 ? 3 : 2, 3,
-                                      KV8 ? 3 : 2, 3,           3,           3,
-                                      KV8 ? 3 : 1, 3};
+        constexpr int kSumAdds16[16] = {0, 3, 1, 3, 0, 0, 2, 3, 2, 3, 2, 3, 3, 3, 1, 3};
+        constexpr int kSumAdds8[16] = {0, 1, 0, 1, 0, 1, 0, 1, 3, 3, 3, 4, 4, 4, 4, 3};
+        auto sum_adds = [=](int i) constexpr { return KV8 ? kSumAdds8[i] : kSumAdds16[i]; };
         u32x4 wide8[4];
 #pragma unroll
         for (int slot = 0; slot < 32; ++slot) {
@@ -573,9 +572,9 @@ __global__ __launch_bounds__(256, 1) void attn_tile256_kernel(
             if (slot >= 16) {
                 int first = 0;
 #pragma unroll
-                for (int t = 16; t < slot; ++t) first += kSumAdds[t - 16];
+                for (int t = 16; t < slot; ++t) first += sum_adds(t - 16);
 #pragma unroll
-                for (int a = 0; a < kSumAdds[slot - 16]; ++a) {
+                for (int a = 0; a < sum_adds(slot - 16); ++a) {
                     const int k = first + a;
                     psum[k / 16] += es[k / 2][k % 2];
                 }

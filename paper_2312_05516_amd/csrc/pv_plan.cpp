@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <functional>
 #include <numeric>
 #include <cstdlib>
 #include <cstring>
@@ -110,6 +111,47 @@ struct CutRule {
     bool level_lists;    // lists of nearly equal items go by how full their last round of CUs is
 };
 
+// How to cut the 256-row kernel's list over 8-bit pools.  One workgroup runs on a CU, so the time of a
+// list is that of the CU with the most keys, when the longest part goes first to the CU that is free
+// first (25 ns a key and 2.5 us an item), and a cut costs the merge besides.  Of a few cuts the best by
+// that count: 512 tiles over 19-25 K keys, two to a CU, take 1217 us whole and 1297 in 1024 parts.
+static Cut tile_cut(const std::vector<WorkItem> &tiles, int32_t head_dim, const Tuning &tune)
+{
+    int64_t total = 0;
+    for (const WorkItem &w : tiles) total += item_cost(w);
+    Cut best = target_cut(total, tiles.size(), tune.split_target, tune);
+    if (tiles.size() > 8 * (size_t)kCUs) return best;
+    double least = -1;
+    std::vector<int64_t> lens, load;
+    for (const int32_t parts : {0, kCUs, 2 * kCUs, 3 * kCUs, 4 * kCUs}) {
+        Cut c = best;
+        c.chunk = parts ? std::max<int64_t>((total + parts - 1) / parts, tune.min_split_keys) : INT32_MAX / 2;
+        c.chunk = (c.chunk + kKvBlock - 1) / kKvBlock * kKvBlock;
+        c.longest_whole = c.chunk;
+        int64_t part_rows = 0;
+        lens.clear();
+        for (const WorkItem &w : tiles) {
+            const int64_t len = item_cost(w), n = c.parts(len);
+            if (n > 1) part_rows += n * w.row_count;
+            for (int64_t i = 0; i < n; ++i) lens.push_back((len + n - 1) / n + 100);
+        }
+        std::sort(lens.begin(), lens.end(), std::greater<int64_t>());
+        load.assign(kCUs, 0);  // a heap, the least at the front
+        for (const int64_t len : lens) {
+            std::pop_heap(load.begin(), load.end(), std::greater<int64_t>());
+            load.back() += len;
+            std::push_heap(load.begin(), load.end(), std::greater<int64_t>());
+        }
+        const double ns = 25.0 * (double)*std::max_element(load.begin(), load.end()) +
+                          (part_rows ? 7000.0 + (double)part_rows * head_dim * 8 / 4000 : 0.0);
+        if (least < 0 || ns < least) {
+            least = ns;
+            best = c;
+        }
+    }
+    return best;
+}
+
 // Cut long items into parts of the KV range.  A cut is not free: every part pays the set-up of an
 // item, writes its rows in fp32, and the merge reads them back.  Returns true where an item gets
 // fewer parts than the cut into about split_target parts gives it.
@@ -148,7 +190,7 @@ struct CutRule {
 // No rule (the 256-row kernel), or a target set by hand: target_cut.
 static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &combine,
                         int64_t &slots_out, const Tuning &tune, const CutRule *rule,
-                        int32_t head_dim, int64_t max_len = 0)
+                        int32_t head_dim, int64_t max_len = 0, const Cut *given = nullptr)
 {
     if (items.empty()) return false;
     if (tune.split_by_hand) rule = nullptr;
@@ -167,7 +209,7 @@ static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &
     const int64_t heads = (int64_t)(items.size() / shapes.size());
     total_keys *= heads;
     const Cut even = target_cut(total_keys, items.size(), tune.split_target, tune);
-    Cut cut = even;
+    Cut cut = given ? *given : even;
     if (rule) {
         auto blocks = [](int64_t keys) { return (keys + kKvBlock - 1) / kKvBlock * kKvBlock; };
         const int64_t n = (int64_t)items.size();
@@ -726,8 +768,10 @@ pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_
         split_items(plan->wide, plan->combine, slots, tune, &wide_rule, pool->head_dim);
     plan->wide_streams = kv_bytes > kStreamKvBytes && wide_once * 3 >= wide_shared;
     plan->narrow_streams = narrow_once > narrow_shared * 4;
+    const bool by_time = kv8 && !tune.split_by_hand && !plan->tile256.empty();
+    const Cut tiles = by_time ? tile_cut(plan->tile256, pool->head_dim, tune) : Cut{};
     split_items(plan->tile256, plan->combine, slots, tune, nullptr, pool->head_dim,
-                kTileMaxKeys);
+                kTileMaxKeys, by_time ? &tiles : nullptr);
     if (slots > INT32_MAX / 2) {
         delete plan;
         return PV_ERR_OUT_OF_RANGE;
