@@ -370,7 +370,7 @@ pv_status pv_norm_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *
  *
  * The pv_pool_desc is that of the rows: dtype is the 16-bit type of q, out, k_new and v_new.  The calls
  * take plans made by pv_plan_create_kv8 and refuse others (PV_ERR_INVALID_ARG), as the calls for 16-bit
- * pools refuse these.  The plan's accessors, upload, timing and pv_plan_check_page_table work as for
+ * pools refuse these (a batch without new tokens apart, which launches nothing).  The plan's accessors, upload, timing and pv_plan_check_page_table work as for
  * other plans; with check_append_unique the latter demands that a page that receives new tokens appears
  * in no other request with new tokens in that page (one page has one scale, which one writer sets).
  */

@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libpv.so")
 OBJ = os.path.join(HERE, "_build")
 
 SOURCES = ["pv_plan.cpp", "pv_lib.hip", "pv_append.hip", "pv_attn_narrow.hip", "pv_attn_wide.hip", "pv_attn_tile256.hip",
-           "pv_swap.hip", "pv_rope.hip", "pv_kv8.hip", "pv_attn_kv8_narrow.hip"]
+           "pv_swap.hip", "pv_rope.hip", "pv_kv8.hip", "pv_attn_kv8_narrow.hip",
+           "pv_attn_kv8_tile256.hip"]
 # packed fp32 VALU forms are switched off for every device compile
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -29,6 +30,7 @@ def _hipcc() -> str:
 
 # kernels with pinned matrix-core instructions: their generated code is kept and scanned (isa_check)
 ISA_CHECKED = ["pv_attn_tile256.hip"]
+ISA_CHECKED_KV8 = ["pv_attn_kv8_tile256.hip"]  # the same kernel over 8-bit pools
 
 
 def isa_path(src: str) -> str:
@@ -37,7 +39,7 @@ def isa_path(src: str) -> str:
 
 def _compile(src: str, extra) -> str:
     obj = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
-    keep = ["-save-temps=obj"] if src in ISA_CHECKED else []
+    keep = ["-save-temps=obj"] if src in ISA_CHECKED + ISA_CHECKED_KV8 else []
     cmd = ([_hipcc()] + FLAGS + keep + list(extra)
            + ["-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj])
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -47,7 +49,7 @@ def _compile(src: str, extra) -> str:
         raise RuntimeError(f"hipcc failed on {src}:\n{msgs}")
     if msgs.strip():
         print(msgs, file=sys.stderr)
-    if src in ISA_CHECKED:
+    if src in ISA_CHECKED + ISA_CHECKED_KV8:
         try:
             from . import isa_check
         except ImportError:  # run as a script: the module sits beside this file

@@ -24,8 +24,7 @@ struct Narrow8Frag {
     uint32_t k_scale, v_scale;
 };
 
-// TWO: see attn_narrow_kernel
-template <typename T, int D, bool TWO>
+template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attn_kv8_narrow_kernel(
     const WorkItem *__restrict__ items, const uint16_t *__restrict__ q, Kv8Ptrs pool,
     const int32_t *__restrict__ page_table, int32_t max_pages, int32_t num_q_heads,
@@ -161,25 +160,16 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_narrow_kernel(
 #pragma unroll
             for (int blk = 0; blk < NB; ++blk) o[blk] *= alpha;
         }
-        constexpr float MOST = TWO ? 0.95f : 1.f;
-        u32x4 pmost[2], prest[2];
+        u32x4 p[2];
 #pragma unroll
-        for (int jj = 0; jj < 8; ++jj) {
-            pmost[jj / 4][jj % 4] = T::pack2(x[2 * jj] * MOST, x[2 * jj + 1] * MOST);
-            if constexpr (TWO) {
-                float m0, m1;
-                T::unpack2(pmost[jj / 4][jj % 4], m0, m1);
-                prest[jj / 4][jj % 4] = T::pack2(x[2 * jj] - m0, x[2 * jj + 1] - m1);
-            }
-        }
+        for (int jj = 0; jj < 8; ++jj) p[jj / 4][jj % 4] = T::pack2(x[2 * jj], x[2 * jj + 1]);
 #pragma unroll
         for (int blk = 0; blk < NB; ++blk) {
             const u32x4 c = f.v[blk];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const vec8 v = as_vec8<T>(decode8<T>(c[2 * half], c[2 * half + 1], v_scale));
-                o[blk] = T::mfma16(v, as_vec8<T>(pmost[half]), o[blk]);
-                if constexpr (TWO) o[blk] = T::mfma16(v, as_vec8<T>(prest[half]), o[blk]);
+                o[blk] = T::mfma16(v, as_vec8<T>(p[half]), o[blk]);
             }
         }
     };
@@ -240,10 +230,8 @@ static void launch_kv8_narrow_t(const pv_plan *plan, const DeviceLists &dl, cons
                                 const Kv8Ptrs &pool, const int32_t *page_table, float scale,
                                 void *out, float *ws_o, float *ws_ml, hipStream_t stream)
 {
-    auto kernel = plan->narrow_two_terms ? attn_kv8_narrow_kernel<T, D, true>
-                                         : attn_kv8_narrow_kernel<T, D, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)plan->narrow.size()), dim3(256), 0, stream, dl.narrow,
-                       (const uint16_t *)q, pool, page_table, plan->max_pages_per_req,
+    hipLaunchKernelGGL((attn_kv8_narrow_kernel<T, D>), dim3((unsigned)plan->narrow.size()), dim3(256), 0,
+                       stream, dl.narrow, (const uint16_t *)q, pool, page_table, plan->max_pages_per_req,
                        plan->num_q_heads, plan->pool.num_kv_heads, plan->group, scale * kLog2e,
                        (uint16_t *)out, ws_o, ws_ml);
 }

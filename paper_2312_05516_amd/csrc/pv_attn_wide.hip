@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
     uint16_t *__restrict__ out, float *__restrict__ ws_o, float *__restrict__ ws_ml,
     int32_t num_reqs, const uint8_t *__restrict__ k_scales, const uint8_t *__restrict__ v_scales)
 {
-    static_assert(!(KV8 && STREAMS), "no such instance");
+    static_assert(!(KV8 && (STREAMS || RENEW)), "no such instance");
     // Keys per block: 32 for head size 128; 64 for head size 64, where 32 keys are only 8
     // matrix-core instructions of a wavefront against about 70 of the vector ALU, a barrier, a
     // test for the maximum and two LDS round trips.  48 requests over 0.1-3 K tokens, 32/8 heads:
@@ -70,8 +70,8 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
     constexpr int PASSES = HALF_BYTES / 4096;   // 16-byte copies per lane for K (same for V)
     constexpr int STAGES = 3;
     // operands of V that are requested while the scores are computed
-    constexpr int V_AHEAD = KV8 && D == 128 ? 6 : PAGES * NB;
-    constexpr int K_AHEAD = KV8 && D == 128 ? 6 : 64;  // and of K before the first product
+    constexpr int V_AHEAD = KV8 && D == 128 ? 5 : PAGES * NB;
+    constexpr int K_AHEAD = KV8 && D == 128 ? 5 : 64;  // and of K before the first product
     typedef typename T::vec8 vec8;
     __shared__ __attribute__((aligned(16))) unsigned char smem[STAGES][2 * HALF_BYTES];
 
@@ -308,23 +308,23 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
     };
     // the thread's place in the page, worked out anew for each block: there is no register to keep it in
     auto in_page = [&]() {
-        int l = (int)lane_bytes;
+        uint32_t l = lane_bytes;
         asm volatile("" : "+v"(l));
-        return (w * 64 % PAGE_THREADS) + (l >> 4);
+        return (uint32_t)(w * 64 % PAGE_THREADS) + (l >> 4);
     };
     auto load8 = [&](int id) {
-        const int at = in_page();
+        const uint32_t at = in_page();
         const int64_t tile = (int64_t)id * num_kv_heads + it.kv_head;
         const uint8_t *k_from = reinterpret_cast<const uint8_t *>(k_pages) + tile * (16 * D);
         const uint8_t *v_from = reinterpret_cast<const uint8_t *>(v_pages) + tile * (16 * D);
-        k8 = load16(k_from + (uint32_t)kv8_k_chunk<D>(at % 16, at / 16));
-        v8 = load16(v_from + (uint32_t)(at * 16));
+        k8 = load16(k_from + (at % 16 / 4 * (4 * D) + at / 16 * 64 + at % 4 * 16));  // kv8_k_chunk
+        v8 = load16(v_from + at * 16);
         k8_scale = k_scales[tile];
         v8_scale = v_scales[tile];
     };
     // block b, whose codes were loaded before, into the stage
     auto widen8 = [&](unsigned char *stage, int b) {
-        const int at = in_page();
+        const uint32_t at = in_page();
         if (it.kv_begin + BK * (b + 1) > item_unmasked) {
             // A NaN among values that some row does not see: zero times it would be NaN in that row too.
             // It is left out, and given to the rows that see it at the end.
@@ -393,16 +393,17 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
         // barrier that publishes the next one
         auto step = [&](int b, auto compute) {
             if constexpr (KV8) {
-                if constexpr (RENEW) to_renewal = (to_renewal == 0 ? renew_blocks : to_renewal) - 1;
                 compute(smem[at], it.kv_begin + BK * b);
                 __builtin_amdgcn_sched_barrier(0);
                 at ^= 1;
+                id1 = page_id8(b + 3);    // on its way while the codes are widened
+                __builtin_amdgcn_sched_barrier(0);
                 widen8(smem[at], b + 1);  // where everyone is done with block b - 1
-                load8(id0);        // block b + 2
-                id0 = page_id8(b + 3);
+                load8(id0);               // block b + 2
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_s_barrier();
-                asm volatile("" : "+s"(id0)::"memory");
+                asm volatile("" : "+s"(id1)::"memory");
+                id0 = id1;
                 return;
             }
             const bool more = b + 2 < nblocks;
@@ -583,13 +584,12 @@ static void launch_wide_t(const pv_plan *plan, const DeviceLists &dl, const void
     const uint32_t q_sign = scale < 0.f ? 0x80008000u : 0u;
     const uint32_t q_keep = c == 0.f ? 0u : 0xFFFFFFFFu;
     if (c == 0.f) c = 1.f;
-    auto kernel = plan->wide_renews ? attn_wide_kernel<T, D, true, false, KV8>
-                                    : attn_wide_kernel<T, D, false, false, KV8>;
-    if constexpr (!KV8) {
-        if (plan->wide_streams)
-            kernel = plan->wide_renews ? attn_wide_kernel<T, D, true, true, false>
-                                       : attn_wide_kernel<T, D, false, true, false>;
-    }
+    auto kernel = attn_wide_kernel<T, D, false, false, KV8>;
+    if constexpr (!KV8)
+        kernel = plan->wide_streams ? (plan->wide_renews ? attn_wide_kernel<T, D, true, true, false>
+                                                         : attn_wide_kernel<T, D, false, true, false>)
+                                    : (plan->wide_renews ? attn_wide_kernel<T, D, true, false, false>
+                                                         : attn_wide_kernel<T, D, false, false, false>);
     hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, stream, dl.wide, (const uint16_t *)q,
                        (const uint16_t *)k_pages, (const uint16_t *)v_pages,
                        page_table, plan->max_pages_per_req, plan->num_q_heads,

@@ -59,6 +59,17 @@ Tuning default_tuning()
     return t;
 }
 
+// Plans for 8-bit pools.  The bandwidth-oriented kernel reads half the bytes for a key, an item of the
+// 128-row kernel holds its slot as long as before, so that fewer small units belong into its launch.
+// Time with one launch over that with two, prompts of 256 tokens and generation steps over 2 K: 10 K
+// steps 0.90, 20 K 0.89, 32 K 0.77 and 1.00, 40 K 0.99, 50 K 1.02, 75 K 1.17, 80 K 1.15, 100 K 1.09.
+Tuning kv8_tuning()
+{
+    Tuning t = default_tuning();
+    t.unify_max_steps = env_int("PV_UNIFY_MAX_STEPS", 40000);
+    return t;
+}
+
 // Whether the full 256-row tiles of a (request, KV head) unit go to the 256-row kernel: that
 // kernel exists for head size 128 and pays off when an item streams many 32-key blocks.
 static bool use_tile256(const pv_pool_desc *pool, const Tuning &tune, int64_t rows_total,
@@ -75,6 +86,7 @@ static int64_t item_cost(const WorkItem &w) { return w.kv_end - w.kv_begin; }
 // into parts of about `chunk` keys, evened out and rounded up to whole blocks.
 struct Cut {
     int64_t chunk, longest_whole, min_keys;
+    int32_t block = kKvBlock;  // keys of the kernel's inner step
     int32_t parts(int64_t len) const
     {
         return len <= longest_whole || len < 2 * min_keys ? 1 : ((int32_t)len - 1) / part_len(len) + 1;
@@ -83,7 +95,7 @@ struct Cut {
     int32_t part_len(int64_t len) const
     {
         const uint32_t keys = (uint32_t)len, n = (keys - 1) / (uint32_t)chunk + 1;
-        return (int32_t)(((keys - 1) / n + kKvBlock) / kKvBlock * kKvBlock);
+        return (int32_t)(((keys - 1) / n + (uint32_t)block) / (uint32_t)block * (uint32_t)block);
     }
 };
 
@@ -109,6 +121,8 @@ struct CutRule {
     int32_t key_ns;      // what a key less in the longest item saves while the GPU is not full
     int32_t always_cut;  // up to this many parts that is not weighed against the merge
     bool level_lists;    // lists of nearly equal items go by how full their last round of CUs is
+    int32_t block;       // parts are whole numbers of so many keys
+    bool whole_counts;   // a cut saves no more than the longest item that it leaves whole lets it
 };
 
 // How to cut the 256-row kernel's list over 8-bit pools.  One workgroup runs on a CU, so the time of a
@@ -211,6 +225,7 @@ static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &
     const Cut even = target_cut(total_keys, items.size(), tune.split_target, tune);
     Cut cut = given ? *given : even;
     if (rule) {
+        cut.block = rule->block;
         auto blocks = [](int64_t keys) { return (keys + kKvBlock - 1) / kKvBlock * kKvBlock; };
         const int64_t n = (int64_t)items.size();
         if (rule->level_lists && n > rule->slots && n < tune.split_target &&
@@ -223,7 +238,7 @@ static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &
             cut.longest_whole = cut.chunk + cut.chunk / 4;
         } else if (rule->always_stretch || n <= rule->slots) {
             auto at_once = [&](int64_t chunk) {
-                const Cut c = {chunk, chunk, cut.min_keys};
+                const Cut c = {chunk, chunk, cut.min_keys, cut.block};
                 int64_t parts = 0;
                 for (const Shape &s : shapes) parts += c.parts(s.len);
                 return parts * heads <= rule->slots;
@@ -257,7 +272,7 @@ static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &
             if (cut.parts(longest) > 1) {
                 const int64_t part_len = cut.part_len(longest);
                 const int64_t after =
-                    few || rule->always_stretch ? std::max(whole, part_len) : part_len;
+                    few || rule->whole_counts ? std::max(whole, part_len) : part_len;
                 if ((longest - after) * rule->key_ns >= 7000 + part_rows * head_dim * 8 / 4000 ||
                     all_parts <= rule->always_cut)
                     break;
@@ -294,7 +309,7 @@ static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &
             continue;
         }
         int64_t part_len = (len + parts - 1) / parts;
-        part_len = (part_len + kKvBlock - 1) / kKvBlock * kKvBlock;
+        part_len = (part_len + cut.block - 1) / cut.block * cut.block;
         parts = (len + part_len - 1) / part_len;
         if (parts <= 1) {
             result.push_back(w);
@@ -757,15 +772,26 @@ pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_
     }
     int64_t slots = 0;
     const bool wide_rows = pool->head_dim == 128;
+    // Over 8-bit pools the narrow kernel takes half the time for a key (one item over 30 K keys 6.3 ns, 3.7
+    // with head size 64) and steps of 64 keys.  Counted with 16 ns, attention call: 32 generation steps
+    // over 2 K, 64/8 heads, 33.8 us in 512 parts (30.1 whole), 16 of 0.5-4 K, 40/40 heads, 78.2 with the
+    // longest cut (73.6 whole).
+    const int32_t narrow_ns = kv8         ? (wide_rows ? 5 : 4)
+                              : wide_rows ? 16
+                                          : (int64_t)plan->narrow.size() > kNarrowSlots ? 12 : 9;
     const CutRule narrow_rule = {
-        kNarrowSlots, wide_rows ? kNarrowSlots * 5 / 4 : 0, kNarrowSlots, 25, false,
-        wide_rows ? 16 : (int64_t)plan->narrow.size() > kNarrowSlots ? 12 : 9, 0, true};
+        kNarrowSlots, wide_rows ? kNarrowSlots * 5 / 4 : 0, kNarrowSlots, 25, false, narrow_ns, 0, true,
+        kv8 ? 2 * kKvBlock : kKvBlock, kv8};
     const CutRule wide_rule = {kWideSlots, kFewWideItems, kFewWideItems, 100, true,
-                               wide_rows ? 31 : 16, wide_rows ? kCUs : 0, false};
+                               wide_rows ? 31 : 16, wide_rows ? kCUs : 0, false, kKvBlock, true};
     plan->narrow_two_terms =
         split_items(plan->narrow, plan->combine, slots, tune, &narrow_rule, pool->head_dim);
     plan->wide_renews =
         split_items(plan->wide, plan->combine, slots, tune, &wide_rule, pool->head_dim);
+    // The kernels for 8-bit pools have neither: over whole lists they are up to 3 % further from 64 bits,
+    // in 16-bit results 1.3 to 1.4 times as far as those' own rounding; two terms would take 6 % of the
+    // time of a list that does not fill the GPU (16 steps over 900 keys, 64/8 heads 13.6 us, 12.8 without).
+    if (kv8) plan->narrow_two_terms = plan->wide_renews = false;
     plan->wide_streams = kv_bytes > kStreamKvBytes && wide_once * 3 >= wide_shared;
     plan->narrow_streams = narrow_once > narrow_shared * 4;
     const bool by_time = kv8 && !tune.split_by_hand && !plan->tile256.empty();
@@ -905,7 +931,7 @@ pv_status pv_plan_create_kv8(const pv_pool_desc *pool, int32_t num_q_heads,
                              int32_t max_pages_per_req, pv_plan **plan)
 {
     return pv::build_plan(pool, num_q_heads, ctx_lens, q_lens, num_reqs, max_pages_per_req,
-                          pv::default_tuning(), plan, true);
+                          pv::kv8_tuning(), plan, true);
 }
 
 int32_t pv_plan_is_kv8(const pv_plan *plan) { return plan ? (plan->kv8 ? 1 : 0) : -1; }

@@ -296,6 +296,7 @@ namespace pv {
 DeviceLists lists_at(const pv_plan *plan, const void *base);
 bool pool_desc_valid(const pv_pool_desc *p, pv_status *why);
 Tuning default_tuning();
+Tuning kv8_tuning();  // of plans for 8-bit pools
 // what every plan demands of a batch; *total_q = its new tokens
 pv_status check_batch(const pv_pool_desc *pool, int32_t num_q_heads, const int32_t *ctx_lens,
                       const int32_t *q_lens, int32_t num_reqs, int32_t max_pages_per_req,

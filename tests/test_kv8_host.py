@@ -186,3 +186,20 @@ def test_pool_of_tensors_that_are_not_contiguous_is_refused():
     t = torch.zeros(64, 2, dtype=torch.uint8)
     with pytest.raises(ValueError):
         pv.Kv8Pool(t[:, 0], t, t, t)
+
+
+def test_generated_code_of_the_256_row_kernel_over_8_bit_pools():
+    """As test_isa_check has it for 16-bit pools: pinned matrix-core instructions, no operand written
+    right in front of one, no spills."""
+    import os
+    from paper_2312_05516_amd import build as pv_build
+    from paper_2312_05516_amd import isa_check
+    for src in pv_build.ISA_CHECKED_KV8:
+        if not os.path.exists(pv_build.isa_path(src)):
+            pv_build.build(verbose=False)
+        with open(pv_build.isa_path(src)) as f:
+            text = f.read()
+        pinned, hazards = isa_check.pinned_mfma_hazards(text)
+        assert pinned >= 64 and hazards == []
+        spills = isa_check.spill_counts(text)
+        assert len(spills) == 2 and all(n == 0 for n in spills.values()), spills
