@@ -203,3 +203,33 @@ def test_generated_code_of_the_256_row_kernel_over_8_bit_pools():
         assert pinned >= 64 and hazards == []
         spills = isa_check.spill_counts(text)
         assert len(spills) == 2 and all(n == 0 for n in spills.values()), spills
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_work_items_cover_every_row_and_key_once(seed):
+    """Of random batches, short and long, in every kernel's list; parts of a row meet, and the merge knows
+    them all."""
+    rng = np.random.default_rng(seed)
+    heads = [(8, 1, 128), (4, 4, 64), (16, 2, 128), (64, 8, 128)][seed % 4]
+    n = int(rng.integers(1, 30))
+    ctx = rng.integers(0, [50, 3000, 30000][seed % 3], n)
+    new = np.where(rng.random(n) < 0.5, 1, rng.integers(0, 600, n))
+    p = pv.plan_create_kv8(pv.pool_desc(70000, heads[1], heads[2], "bf16"), heads[0], ctx, new, 2000)
+    group = heads[0] // heads[1]
+    rows = {(r, h): [[] for _ in range(int(new[r]) * group)] for r in range(n) for h in range(heads[1])}
+    parts = 0
+    for kind, most in ((0, 16), (1, 128), (3, 256)):
+        for i in range(pv.plan_num_work_items(p, kind)):
+            r, h, first, count, lo, hi, at, of = (int(x) for x in pv.plan_work_item(p, kind, i))
+            assert 0 < count <= most and (kind != 3 or count == 256)
+            assert lo < hi and lo % 32 == 0 and 0 <= at < of and (of > 1 or lo == 0)
+            parts += of > 1
+            for row in range(first, first + count):
+                rows[r, h][row].append((lo, hi))
+    merged = sum(int(pv.plan_work_item(p, 2, i)[7]) for i in range(pv.plan_num_work_items(p, 2)))
+    assert merged == parts
+    for (r, h), each in rows.items():
+        for row, spans in enumerate(each):
+            spans.sort()
+            assert spans and spans[0][0] == 0 and all(a[1] == b[0] for a, b in zip(spans, spans[1:]))
+            assert spans[-1][1] >= ctx[r] + row // group + 1  # and sees its own token
