@@ -75,13 +75,17 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_narrow_kernel(
     const int k_at = g * 64 + (q16 & 3) * 16;           // + tile * 4 * D + 64 dimensions * 256
     const int v_at = q16 * 16;                          // + blk * 256
 
+    // page ids of a block, fetched a block before its K and V so that these do not wait for them
+    int ids[4];
+    auto page_ids = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ids[i] = pt[min(pg0 + 4 * b + i, last_pg)];
+    };
     auto load_block = [&](Narrow8Frag<D> &f, int b) {
         int64_t tile[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int pg = pg0 + 4 * b + i;
-            tile[i] = (int64_t)pt[pg <= last_pg ? pg : last_pg] * num_kv_heads + it.kv_head;
-        }
+        for (int i = 0; i < 4; ++i) tile[i] = (int64_t)ids[i] * num_kv_heads + it.kv_head;
+        page_ids(b + NW);
         const int64_t k01 = k_page & 1 ? tile[1] : tile[0], k23 = k_page & 1 ? tile[3] : tile[2];
         const int64_t v01 = g & 1 ? tile[1] : tile[0], v23 = g & 1 ? tile[3] : tile[2];
         const int64_t kt = k_page & 2 ? k23 : k01, vt = g & 2 ? v23 : v01;
@@ -177,6 +181,7 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_narrow_kernel(
     {
         Narrow8Frag<D> fa, fb;
         int b = w;
+        page_ids(b);
         if (b < nblocks) load_block(fa, b);
         while (b < nblocks) {
             int nxt = b + NW;
