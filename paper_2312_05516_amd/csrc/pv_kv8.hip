@@ -12,7 +12,13 @@
 // are 4 KiB, 64 bytes a lane, so that the maximum over the block takes six lane exchanges and no LDS.
 // K: lane = (slot, 16 dimensions of either half), whose codes are the pool's 16-byte chunks and
 // which holds both partners of a rotation.  V: lane = two dimensions of all 16 slots, so that the
-// transposition into the pool's runs of 16 slots is byte permutes inside a lane.
+// transposition into the pool's runs of 16 slots is byte permutes inside a lane.  Queries, which are not
+// quantised: D/16 lanes a row, 16 bytes of either half side by side (32 bytes a lane, as K has them: 40.0 us
+// for 4.4 K tokens, 64/8 heads, 38.4 so).
+//
+// Measured: 8 prompts, 6.5 K tokens, 40 KV heads, 201 MB in 38.2 us = 5.25 TB/s (a device copy of 1 GiB:
+// 5.2); reading 70 K tokens of 8 heads back, 427 MB in 85.1 us = 5.0 TB/s; norms and rotation in front, 4.4 K
+// tokens, 64/8 heads, 172 MB in 33.7 us = 5.1 TB/s; 256 generation steps 4.2 us, launch and latency.
 #include "pv_kv8.h"
 
 namespace pv {
@@ -273,30 +279,95 @@ __device__ __forceinline__ void append_v8(const AppendGroup &g, int h, int heads
     }
 }
 
-// A token's queries of HB heads, normalised and rotated: the lane's rows begin `row` elements into the
-// array, `step` elements apart; `heads` of them exist (at least one).
-template <typename T, int D, int STYLE, int HB>
-__device__ __forceinline__ void rotate_q(int64_t row, int64_t step, int heads, int c,
-                                         const uint16_t *q_in, uint16_t *q_out,
-                                         const uint16_t *weight, float eps, const float *cs)
-{
-    u32x4 rows[HB][4], w[4];
+// Rows of queries, normalised and rotated.  A lane holds chunks c and c + D/16 (of 8 dimensions) of a
+// row, partners of a rotation, so that the D/16 lanes of a row read and write 16 bytes side by side.
+template <int D, int STYLE>
+struct ChunkAngles {
+    f32x4 c[2], s[2];
+    __device__ __forceinline__ void load(const float *cs, int lane_c)
+    {
 #pragma unroll
-    for (int i = 0; i < HB; ++i)
-        load_halves<D, false>(rows[i], q_in + row + (i < heads ? i : 0) * step, c);
-    Angles<D, STYLE> angle;
-    angle.load(cs, c);
-    if (weight) load_halves<D, false>(w, weight, c);
-#pragma unroll
-    for (int i = 0; i < HB; ++i) {
-        if (i >= heads) break;
-        norm_rotate<T, D, STYLE>(rows[i], weight != nullptr, w, eps, angle);
-        uint16_t *to = q_out + row + i * step + 16 * c;
-        *reinterpret_cast<u32x4 *>(to) = rows[i][0];
-        *reinterpret_cast<u32x4 *>(to + 8) = rows[i][1];
-        *reinterpret_cast<u32x4 *>(to + D / 2) = rows[i][2];
-        *reinterpret_cast<u32x4 *>(to + D / 2 + 8) = rows[i][3];
+        for (int k = 0; k < 2; ++k) {
+            const float *at = cs + (STYLE == 1 ? 8 * lane_c + 4 * k : 4 * lane_c + k * (D / 4));
+            c[k] = *reinterpret_cast<const f32x4 *>(at);
+            s[k] = *reinterpret_cast<const f32x4 *>(at + D / 2);
+        }
     }
+};
+
+template <typename T, int D, int STYLE>
+__device__ __forceinline__ void norm_rotate_chunks(u32x4 (&raw)[2], bool norm,
+                                                   const u32x4 (&weight)[2], float eps,
+                                                   const ChunkAngles<D, STYLE> &angle)
+{
+    float x[2][8], y[2][8];
+    unpack8<T>(raw[0], x[0]);
+    unpack8<T>(raw[1], x[1]);
+    if (norm) {
+        const float r = norm_factor<D>(sum_squares(x[0]) + sum_squares(x[1]), eps);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float w[8];
+            unpack8<T>(weight[i], w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] * r * w[e];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (STYLE == 1)  // dimensions i and i + D/2
+                rotate_pair(x[0][4 * k + e], x[1][4 * k + e], angle.c[k][e], angle.s[k][e],
+                            y[0][4 * k + e], y[1][4 * k + e]);
+            else  // dimensions 2i and 2i + 1
+                rotate_pair(x[k][2 * e], x[k][2 * e + 1], angle.c[k][e], angle.s[k][e], y[k][2 * e],
+                            y[k][2 * e + 1]);
+        }
+    raw[0] = pack8<T>(y[0]);
+    raw[1] = pack8<T>(y[1]);
+}
+
+// HEADS heads of TOKENS tokens a lane (of one wavefront): token t of the lane is j0 + t * 64 / (D/16) of the
+// group if that exists, `row` the element of its head 0 there, heads `step` elements apart.
+template <typename T, int D, int STYLE, int HEADS, int TOKENS, bool STREAM>
+__device__ __forceinline__ void rotate_q(const AppendGroup &g, int j0, int64_t token_step,
+                                         int64_t row, int64_t step, int heads, const uint16_t *q_in,
+                                         uint16_t *q_out, const uint16_t *weight, float eps,
+                                         const float *cos_sin)
+{
+    constexpr int LPR = D / 16;
+    const int c = lane_id() % LPR;
+    u32x4 rows[TOKENS][HEADS][2], w[2];
+    ChunkAngles<D, STYLE> angle[TOKENS];
+    int64_t at[TOKENS];
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+        const int j = min(j0 + t * (64 / LPR), g.count - 1);
+        at[t] = row + j * token_step + 8 * c;
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            const uint16_t *from = q_in + at[t] + (i < heads ? i : 0) * step;
+            rows[t][i][0] = load16_as<STREAM>(from);
+            rows[t][i][1] = load16_as<STREAM>(from + D / 2);
+        }
+        angle[t].load(cos_sin + (int64_t)(g.t_begin + j) * D, c);
+    }
+    if (weight) {
+        w[0] = load16(weight + 8 * c);
+        w[1] = load16(weight + D / 2 + 8 * c);
+    }
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t)
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            norm_rotate_chunks<T, D, STYLE>(rows[t][i], weight != nullptr, w, eps, angle[t]);
+            if (i < heads && j0 + t * (64 / LPR) < g.count) {
+                uint16_t *to = q_out + at[t] + i * step;
+                *reinterpret_cast<u32x4 *>(to) = rows[t][i][0];
+                *reinterpret_cast<u32x4 *>(to + D / 2) = rows[t][i][1];
+            }
+        }
 }
 
 // Grid: (append groups, blocks of heads): the two wavefronts store K and V of HB KV heads (twice as
@@ -314,13 +385,12 @@ __global__ __launch_bounds__(128) void kv8_append_kernel(
     const int w = wave_id();
     const int kv_blocks = (num_kv_heads + HEADS - 1) / HEADS;
     if (STYLE >= 0 && (int)blockIdx.y >= kv_blocks) {
-        constexpr int LPT = D / 32;
-        const int h = (2 * ((int)blockIdx.y - kv_blocks) + w) * HEADS + Side<D>::head();
-        const int j = Side<D>::lane() / LPT, c = Side<D>::lane() % LPT;
-        if (h >= num_q_heads || j >= g.count) return;
-        rotate_q<T, D, STYLE < 0 ? 0 : STYLE, HB>(
-            ((int64_t)(g.q_row + j) * num_q_heads + h) * D, SH * D, (num_q_heads - h + SH - 1) / SH, c,
-            q_in, q_out, q_weight, eps, cos_sin + (int64_t)(g.t_begin + j) * D);
+        const int h = (2 * ((int)blockIdx.y - kv_blocks) + w) * HEADS;
+        if (h >= num_q_heads) return;
+        rotate_q<T, D, STYLE < 0 ? 0 : STYLE, HEADS, D / 64, STREAM>(
+            g, lane_id() / (D / 16), (int64_t)num_q_heads * D,
+            ((int64_t)g.q_row * num_q_heads + h) * D, D, num_q_heads - h, q_in, q_out, q_weight, eps,
+            cos_sin);
         return;
     }
     const int h = (int)blockIdx.y * HEADS, heads = min(HEADS, num_kv_heads - h);
@@ -352,11 +422,13 @@ __global__ __launch_bounds__(64) void kv8_step_kernel(
     const int k_blocks = (num_kv_heads + KH - 1) / KH, v_blocks = (num_kv_heads + VH - 1) / VH;
     int y = (int)blockIdx.y;
     if (STYLE >= 0 && y >= k_blocks + v_blocks) {
-        const int h = (y - k_blocks - v_blocks) * KH + lane / LPT, c = lane % LPT;
-        if (h >= num_q_heads) return;
-        rotate_q<T, D, STYLE < 0 ? 0 : STYLE, 1>(((int64_t)g.q_row * num_q_heads + h) * D, 0, 1, c,
-                                                 q_in, q_out, q_weight, eps,
-                                                 cos_sin + (int64_t)g.t_begin * D);
+        const int h0 = (y - k_blocks - v_blocks) * KH;
+        const int first = lane / (VL / 2), each = 64 / (VL / 2);
+        const int h = min(h0 + first, num_q_heads - 1);
+        const int mine = h0 + first < num_q_heads ? (num_q_heads - h + each - 1) / each : 0;
+        rotate_q<T, D, STYLE < 0 ? 0 : STYLE, 2, 1, false>(
+            g, 0, 0, ((int64_t)g.q_row * num_q_heads + h) * D, each * D, mine, q_in, q_out, q_weight,
+            eps, cos_sin);
         return;
     }
     const int64_t page = page_table[(int64_t)g.req * max_pages + (g.t_begin >> 4)];
@@ -549,10 +621,13 @@ __global__ __launch_bounds__(128) void kv8_read_kernel(
 //  * Batches of one token a request take the kernel for them: 256 requests, 8 KV heads 4.5 (5.5 with the
 //    kernel for pages), 40 heads 12.2 (15.7).
 //  * With rotation more than 32 MiB of rows take two heads a wavefront, which share the angles: 6
-//    prompts, 40/40 heads, 4.2 K tokens 54.4 (one: 58.9), 8 of 300, 64/8 heads 22.7 (25.0), but 2 of 100
+//    prompts, 40/40 heads, 4.8 K tokens 53.3 (one: 56.0), 8 of 300, 64/8 heads 21.1 (22.8), but 2 of 100
 //    5.6 (4.3).  Without rotation one head is ahead (6 K tokens, 40 heads: 39.7, two 41.4).
-//  * Without rotation more than 64 MiB of rows are read with the streaming hint: 6 K tokens, 40 heads 36.0
-//    (39.7), 4 K 25.3 (26.9), 3 K 24.3 (22.3).  With rotation it makes no difference to 3 %.
+//  * More than 64 MiB of rows, with rotation more than 48 and head size 128, are read with the streaming
+//    hint.  Without rotation 6 K tokens, 40 heads 36.0 (39.7 without the hint), 4 K 25.3 (26.9), 3 K 24.3
+//    (22.3).  With it 4.4 K tokens, 64/8 heads 33.7 (38.4), 3.2 K 25.9 (29.0), 2.4 K 21.1 (21.2); 4.8 K, 40/40
+//    heads 50.0 (53.3).  Head size 64, whose half rows are half a cache line: 22 K tokens, 32/8 heads 59.4
+//    (56.8).
 template <typename T, int D, int STYLE>
 static void launch_append8_t(const pv_plan *plan, const DeviceLists &dl, const NormRope &nr,
                              const void *k_new, const void *v_new, const int32_t *page_table,
@@ -562,7 +637,8 @@ static void launch_append8_t(const pv_plan *plan, const DeviceLists &dl, const N
     const int64_t row_bytes = (int64_t)plan->total_q * (2 * hkv + hq) * D * 2;
     const bool steps = (int32_t)plan->append_groups.size() == plan->total_q;  // one token a group
     const bool two = STYLE >= 0 && row_bytes > kStreamBytes;
-    const bool streams = STYLE < 0 && row_bytes > 2 * kStreamBytes;
+    const bool streams = STYLE < 0 ? row_bytes > 2 * kStreamBytes
+                                   : D == 128 && 2 * row_bytes > 3 * kStreamBytes;
     constexpr int KH = 64 / (D / 32), VH = 64 / (D / 8);
     const int heads = (two ? 2 : 1) * (128 / D);
     const int blocks = steps ? (hkv + KH - 1) / KH + (hkv + VH - 1) / VH + (hq + KH - 1) / KH
@@ -573,6 +649,7 @@ static void launch_append8_t(const pv_plan *plan, const DeviceLists &dl, const N
         if (!steps && streams) kernel = kv8_append_kernel<T, D, STYLE, 1, true>;
     } else {
         if (!steps && two) kernel = kv8_append_kernel<T, D, STYLE, 2, false>;
+        if (!steps && streams) kernel = kv8_append_kernel<T, D, STYLE, 2, true>;
     }
     hipLaunchKernelGGL(kernel, grid, dim3(steps ? 64 : 128), 0, stream,
                        dl.append_groups, (const uint16_t *)nr.q_in, (uint16_t *)nr.q_out,
