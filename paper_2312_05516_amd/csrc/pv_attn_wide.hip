@@ -301,7 +301,10 @@ __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
     // below it nothing is masked for any row of the item
     const int item_unmasked = min(it.ctx + (int)rows.tok0 + 1, it.kv_end);
     __shared__ int left_out;
-    if (KV8 && threadIdx.x == 0) left_out = 0;
+    if constexpr (KV8) {
+        if (threadIdx.x == 0) left_out = 0;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // in front of the barrier before its first use
+    }
     u32x4 k8, v8;
     uint32_t k8_scale, v8_scale;
     auto page_id8 = [&](int b) {
