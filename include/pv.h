@@ -171,7 +171,8 @@ pv_status pv_plan_work_item(const pv_plan *plan, int32_t kind, int32_t index, in
  * bandwidth-oriented kernel takes its probabilities in two 16-bit terms, 2 = it reads K/V with the
  * streaming hint, 4 = items of the matrix-core kernel (128 rows) renew their reference maximum, 8 =
  * items of it that alone read their K/V do so with the streaming hint (the kernel still excepts pages
- * that requests share), 16 = the 256-row kernel applies the scale to the scores, not the queries.  -1 for NULL. */
+ * that requests share), 16 = the 256-row kernel applies the scale to the scores, not the queries (over 8-bit pools these
+ * kernels have 2 and 16 always and no other variant).  -1 for NULL. */
 int32_t pv_plan_kernel_variants(const pv_plan *plan);
 
 /* Host-side check of a page table against the plan (host copy of the table, row stride
@@ -340,7 +341,8 @@ pv_status pv_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *q_out
  * head) becomes
  *     y = x * w / sqrt(mean(x^2) + eps)
  * and is then rotated and stored as by pv_rope_kv_append_planned; V is moved as there.  fp32
- * throughout (the sum of squares too), rounded to the 16-bit type once, behind the rotation.
+ * throughout (the sum of squares too; a bf16 row for which it is past fp32 becomes zeros), rounded to the
+ * 16-bit type once, behind the rotation.
  *   q_weight, k_weight : device [D] of the pool's type, 16-byte aligned, shared by all heads; NULL =
  *                        rows of that kind are not normalised, only rotated
  *   eps                : finite and positive, else PV_ERR_INVALID_ARG (a row of zeros stays zero)
@@ -370,9 +372,10 @@ pv_status pv_norm_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *
  *
  * The pv_pool_desc is that of the rows: dtype is the 16-bit type of q, out, k_new and v_new.  The calls
  * take plans made by pv_plan_create_kv8 and refuse others (PV_ERR_INVALID_ARG), as the calls for 16-bit
- * pools refuse these (a batch without new tokens apart, which launches nothing).  The plan's accessors, upload, timing and pv_plan_check_page_table work as for
- * other plans; with check_append_unique the latter demands that a page that receives new tokens appears
- * in no other request with new tokens in that page (one page has one scale, which one writer sets).
+ * pools refuse these (a batch without new tokens apart, which launches nothing).  The plan's accessors,
+ * upload, timing and pv_plan_check_page_table work as for other plans; with check_append_unique the latter demands that a page that receives new tokens appears
+ * in no other request with new tokens in that page (one page has one scale, which one writer sets).  A
+ * request that only reads such a page sees its earlier codes as the writer leaves them.
  */
 typedef struct {
     void *k, *v;                  /* device, 16-byte aligned */
@@ -435,7 +438,8 @@ pv_status pv_kv8_read_planned(pv_plan *plan, const pv_kv8_pool *pool, const int3
  * Multi-token paged attention over 8-bit pools: pv_multi_token_paged_attn_planned with K, V = code *
  * 2^e.  Codes are widened to the 16-bit type on the way to the matrix cores, which is exact; everything
  * behind that is as there (scores, softmax and sums in fp32, probabilities and results rounded to
- * 16 bits).  Arguments, workspace and launches as there.
+ * 16 bits).  Arguments, workspace and launches as there.  A NaN code reaches the rows that see its
+ * position and no others.
  */
 pv_status pv_kv8_multi_token_paged_attn_planned(pv_plan *plan, const void *q,
                                                 const pv_kv8_pool *pool,

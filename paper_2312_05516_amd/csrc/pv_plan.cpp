@@ -967,6 +967,7 @@ int32_t pv_plan_num_work_items(const pv_plan *plan, int32_t kind)
 int32_t pv_plan_kernel_variants(const pv_plan *plan)
 {
     if (!plan) return -1;
+    if (plan->kv8) return (plan->narrow.empty() ? 0 : 2) | (plan->tile256.empty() ? 0 : 16);
     return (plan->narrow_two_terms ? 1 : 0) | (plan->narrow_streams ? 2 : 0) |
            (plan->wide_renews ? 4 : 0) | (plan->wide_streams ? 8 : 0) |
            (plan->tile_scales_scores ? 16 : 0);

@@ -382,6 +382,28 @@ def test_another_stream_and_timing():
     assert max(run.pv.plan_kernel_ms(run.plan, k) for k in (0, 1)) > 0
 
 
+def test_one_plan_on_two_streams_at_once():
+    """Two layers at a time: pools, results and workspaces of their own, lists and page table shared."""
+    import torch
+    b = _batch([7000, 300, 20], [1, 1, 60], (8, 2, 128), "bf16")
+    run = R.Run(b)
+    layers = [(R.to_dev(p), q) for p, q in (R.filled(b, 212), R.filled(b, 214))]
+    want = [run.attend(dev, q) for dev, q in layers]
+    assert not np.array_equal(*want)
+    streams = [torch.cuda.Stream() for _ in layers]
+    args = [(H.to_dev_bits(q, "bf16"), torch.empty_like(run.ws)) for _, q in layers]
+    outs = [[torch.empty_like(q) for _ in range(8)] for q, _ in args]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for (dev, _), (q, ws), out, stream in zip(layers, args, outs, streams):
+            run.pv.kv8_multi_token_paged_attn_planned(run.plan, q, dev, run.table, b.scale, out[i], ws,
+                                                      stream=stream)
+    torch.cuda.synchronize()
+    for w, out in zip(want, outs):
+        for o in out:
+            assert np.array_equal(H.bits_to_f64(H.from_dev_bits(o), "bf16"), w)
+
+
 @pytest.mark.parametrize("ctx,new", [([300, 20], [1, 60]), ([7000], [1])])
 def test_captured_and_replayed(ctx, new):
     """Append, attention and reading back in one graph; replays with other rows in the same buffers."""

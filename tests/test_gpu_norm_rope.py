@@ -139,6 +139,18 @@ def test_rows_of_zeros_and_of_extreme_size(dtype):
         _close(k_rows, k, w[1], b, "half", eps)
 
 
+def test_the_smallest_and_largest_eps():
+    """A row of zeros stays zero, and one of finite values finite, however small or large eps is."""
+    b = _batch((2, 2, 128), "bf16")
+    q, k, v, w = _inputs(b)
+    q[0], k[1] = 0, 0
+    for eps in (1e-45, 1e-39, 1e38):
+        q_out, k_rows, _, _ = _call16(b, q, k, v, w, "half", eps=eps)
+        assert not (q_out[0] & 0x7FFF).any() and not (k_rows[1] & 0x7FFF).any()
+        _close(q_out, q, w[0], b, "half", eps)
+        _close(k_rows, k, w[1], b, "half", eps)
+
+
 def test_nan_stays_in_its_row():
     b = _batch((2, 2, 128), "bf16")
     q, k, v, w = _inputs(b)
@@ -165,7 +177,7 @@ def _same_or_next(got, want, exact):
 @pytest.mark.parametrize("weights", ["both", "none"])
 @pytest.mark.parametrize("heads,dtype", [((6, 3, 128), "bf16"), ((33, 11, 64), "f16"),
                                          ((8, 1, 128), "f16"), ((5, 5, 64), "bf16")])
-@pytest.mark.parametrize("batch", ["mixed", "steps", "many"])
+@pytest.mark.parametrize("batch", ["mixed", "steps", "many", "more"])
 def test_into_8_bit_pools_is_norm_rotation_and_append(heads, dtype, weights, style, batch):
     """What the call for 16-bit pools rounds, quantised as the append does: bit for bit in bf16 with norms.
     In f16 the last multiply-add and the rounding to 16 bits may be one instruction, which rounds once
@@ -176,8 +188,8 @@ def test_into_8_bit_pools_is_norm_rotation_and_append(heads, dtype, weights, sty
     import torch
     if batch == "steps":
         b = _batch(heads, dtype, (0, 1, 15, 40, 31), (1, 1, 1, 1, 1))
-    elif batch == "many":  # over 32 MiB of rows: two heads a wavefront
-        rows = (33 << 20) // (2 * heads[2] * (heads[0] + 2 * heads[1]))
+    elif batch in ("many", "more"):  # over 32 MiB of rows: two heads a wavefront; over 48: streaming loads
+        rows = ((33 if batch == "many" else 50) << 20) // (2 * heads[2] * (heads[0] + 2 * heads[1]))
         b = _batch(heads, dtype, (0, 5), (rows - 60, 61))
     else:
         b = _batch(heads, dtype)

@@ -69,6 +69,8 @@ def test_plans_for_8_bit_pools():
     for ctx, new, kind in (((20000,) * 8, (512,) * 8, 3), ((900, 300), (100, 90), 1), ((900, 300), (1, 1), 0)):
         q = _plan(ctx=ctx, new=new, heads=(64, 8, 128), max_pages=2000, pages=20000)
         assert [pv.plan_num_work_items(q, k) > 0 for k in (0, 1, 3)] == [kind == k for k in (0, 1, 3)]
+        variants = pv.plan_kernel_variants(q)  # of those kernels the only ones there are
+        assert variants == {0: 2, 1: 0, 3: 16}[kind]
     for bad, status in (((pv.pool_desc(4, 2, 96, "f16"), 4, [1], [1], 4), UNSUPPORTED),
                         ((pv.pool_desc(4, 2, 64, "f16"), 3, [1], [1], 4), INVALID),
                         ((pv.pool_desc(4, 2, 64, "f16"), 4, [-1], [1], 4), INVALID),
@@ -203,6 +205,15 @@ def test_generated_code_of_the_256_row_kernel_over_8_bit_pools():
         assert pinned >= 64 and hazards == []
         spills = isa_check.spill_counts(text)
         assert len(spills) == 2 and all(n == 0 for n in spills.values()), spills
+
+
+def test_tiles_over_long_contexts_have_room_for_their_page_ids(monkeypatch):
+    """The 256-row kernel keeps the page ids of an item in LDS, 8192 of them, however the list is cut."""
+    monkeypatch.setenv("PV_TILE_MIN_KEYS", "64")
+    for ctx in ((300000,), (400000, 20), (131072 - 256,), (131072,), (1000000,) * 3):
+        p = _plan(ctx=ctx, new=(256,) * len(ctx), heads=(8, 1, 128), max_pages=70000, pages=200000)
+        items = [pv.plan_work_item(p, 3, i) for i in range(pv.plan_num_work_items(p, 3))]
+        assert len(items) >= 8 * len(ctx) and all(0 < int(w[5]) - int(w[4]) <= 8192 * 16 for w in items)
 
 
 @pytest.mark.parametrize("seed", range(12))
