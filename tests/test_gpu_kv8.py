@@ -308,6 +308,29 @@ def test_page_order_and_shared_pages_change_nothing(new):
     _check_attention(b, p, q, table=shared)
 
 
+def test_pages_swapped_out_and_in():
+    """A block of head size 128 has the bytes of a 16-bit block of head size 64, so the page copy moves 8-bit
+    pages under a description of those; scales are a byte for each block beside them."""
+    import torch
+    b = _batch([200, 90], [1, 40], (8, 2, 128), "bf16")
+    p, q = R.filled(b, 190)
+    run, dev = R.Run(b), R.to_dev(p)
+    want = run.attend(dev, q)
+    half = run.pv.pool_desc(b.num_pages, 2, 64, "bf16")
+    src = torch.arange(b.num_pages, dtype=torch.int32, device="cuda")
+    staging = torch.empty(b.num_pages * 2 * 2 * 2048, dtype=torch.uint8, pin_memory=True)
+    run.pv.pages_gather(half, dev.k, dev.v, src, b.num_pages, staging)
+    torch.cuda.synchronize()
+    order = np.random.default_rng(2).permutation(b.num_pages).astype(np.int32)
+    back = R.to_dev(R.Pools(b, "random", seed=13))
+    to = torch.from_numpy(order).cuda()
+    run.pv.pages_scatter(half, staging, to, b.num_pages, back.k, back.v)
+    for n in ("k_scales", "v_scales"):
+        getattr(back, n).view(b.num_pages, 2)[to.long()] = getattr(dev, n).view(b.num_pages, 2)
+    table = np.where(b.page_table >= 0, order[b.page_table], -1)
+    assert np.array_equal(want, R.Run(b, table).attend(back, q))
+
+
 def test_offsets_past_32_bits():
     """Pools of 4.3 GB: pages whose codes lie behind 2^32."""
     import torch
