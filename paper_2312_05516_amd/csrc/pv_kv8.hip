@@ -20,6 +20,7 @@
 // 5.2); reading 70 K tokens of 8 heads back, 427 MB in 85.1 us = 5.0 TB/s; norms and rotation in front, 4.4 K
 // tokens, 64/8 heads, 172 MB in 33.7 us = 5.1 TB/s; 256 generation steps 4.2 us, launch and latency.
 #include "pv_kv8.h"
+#include "pv_norm_rope.h"
 
 namespace pv {
 
@@ -279,97 +280,6 @@ __device__ __forceinline__ void append_v8(const AppendGroup &g, int h, int heads
     }
 }
 
-// Rows of queries, normalised and rotated.  A lane holds chunks c and c + D/16 (of 8 dimensions) of a
-// row, partners of a rotation, so that the D/16 lanes of a row read and write 16 bytes side by side.
-template <int D, int STYLE>
-struct ChunkAngles {
-    f32x4 c[2], s[2];
-    __device__ __forceinline__ void load(const float *cs, int lane_c)
-    {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float *at = cs + (STYLE == 1 ? 8 * lane_c + 4 * k : 4 * lane_c + k * (D / 4));
-            c[k] = *reinterpret_cast<const f32x4 *>(at);
-            s[k] = *reinterpret_cast<const f32x4 *>(at + D / 2);
-        }
-    }
-};
-
-template <typename T, int D, int STYLE>
-__device__ __forceinline__ void norm_rotate_chunks(u32x4 (&raw)[2], bool norm,
-                                                   const u32x4 (&weight)[2], float eps,
-                                                   const ChunkAngles<D, STYLE> &angle)
-{
-    float x[2][8], y[2][8];
-    unpack8<T>(raw[0], x[0]);
-    unpack8<T>(raw[1], x[1]);
-    if (norm) {
-        const float r = norm_factor<D>(sum_squares(x[0]) + sum_squares(x[1]), eps);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float w[8];
-            unpack8<T>(weight[i], w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] * r * w[e];
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (STYLE == 1)  // dimensions i and i + D/2
-                rotate_pair(x[0][4 * k + e], x[1][4 * k + e], angle.c[k][e], angle.s[k][e],
-                            y[0][4 * k + e], y[1][4 * k + e]);
-            else  // dimensions 2i and 2i + 1
-                rotate_pair(x[k][2 * e], x[k][2 * e + 1], angle.c[k][e], angle.s[k][e], y[k][2 * e],
-                            y[k][2 * e + 1]);
-        }
-    raw[0] = pack8<T>(y[0]);
-    raw[1] = pack8<T>(y[1]);
-}
-
-// HEADS heads of TOKENS tokens a lane (of one wavefront): token t of the lane is j0 + t * 64 / (D/16) of the
-// group if that exists, `row` the element of its head 0 there, heads `step` elements apart.
-template <typename T, int D, int STYLE, int HEADS, int TOKENS, bool STREAM>
-__device__ __forceinline__ void rotate_q(const AppendGroup &g, int j0, int64_t token_step,
-                                         int64_t row, int64_t step, int heads, const uint16_t *q_in,
-                                         uint16_t *q_out, const uint16_t *weight, float eps,
-                                         const float *cos_sin)
-{
-    constexpr int LPR = D / 16;
-    const int c = lane_id() % LPR;
-    u32x4 rows[TOKENS][HEADS][2], w[2];
-    ChunkAngles<D, STYLE> angle[TOKENS];
-    int64_t at[TOKENS];
-#pragma unroll
-    for (int t = 0; t < TOKENS; ++t) {
-        const int j = min(j0 + t * (64 / LPR), g.count - 1);
-        at[t] = row + j * token_step + 8 * c;
-#pragma unroll
-        for (int i = 0; i < HEADS; ++i) {
-            const uint16_t *from = q_in + at[t] + (i < heads ? i : 0) * step;
-            rows[t][i][0] = load16_as<STREAM>(from);
-            rows[t][i][1] = load16_as<STREAM>(from + D / 2);
-        }
-        angle[t].load(cos_sin + (int64_t)(g.t_begin + j) * D, c);
-    }
-    if (weight) {
-        w[0] = load16(weight + 8 * c);
-        w[1] = load16(weight + D / 2 + 8 * c);
-    }
-#pragma unroll
-    for (int t = 0; t < TOKENS; ++t)
-#pragma unroll
-        for (int i = 0; i < HEADS; ++i) {
-            norm_rotate_chunks<T, D, STYLE>(rows[t][i], weight != nullptr, w, eps, angle[t]);
-            if (i < heads && j0 + t * (64 / LPR) < g.count) {
-                uint16_t *to = q_out + at[t] + i * step;
-                *reinterpret_cast<u32x4 *>(to) = rows[t][i][0];
-                *reinterpret_cast<u32x4 *>(to + D / 2) = rows[t][i][1];
-            }
-        }
-}
-
 // Grid: (append groups, blocks of heads): the two wavefronts store K and V of HB KV heads (twice as
 // many of head size 64), or, behind those, rotate the queries of as many query heads each.
 template <typename T, int D, int STYLE, int HB, bool STREAM>
@@ -422,13 +332,11 @@ __global__ __launch_bounds__(64) void kv8_step_kernel(
     const int k_blocks = (num_kv_heads + KH - 1) / KH, v_blocks = (num_kv_heads + VH - 1) / VH;
     int y = (int)blockIdx.y;
     if (STYLE >= 0 && y >= k_blocks + v_blocks) {
-        const int h0 = (y - k_blocks - v_blocks) * KH;
-        const int first = lane / (VL / 2), each = 64 / (VL / 2);
-        const int h = min(h0 + first, num_q_heads - 1);
-        const int mine = h0 + first < num_q_heads ? (num_q_heads - h + each - 1) / each : 0;
+        static_assert(StepHeads<D>::kHeads == KH, "queries go in as many blocks as keys");
+        const StepHeads<D> mine((y - k_blocks - v_blocks) * KH, num_q_heads);
         rotate_q<T, D, STYLE < 0 ? 0 : STYLE, 2, 1, false>(
-            g, 0, 0, ((int64_t)g.q_row * num_q_heads + h) * D, each * D, mine, q_in, q_out, q_weight,
-            eps, cos_sin);
+            g, 0, 0, ((int64_t)g.q_row * num_q_heads + mine.first) * D, StepHeads<D>::kEach * D,
+            mine.count, q_in, q_out, q_weight, eps, cos_sin);
         return;
     }
     const int64_t page = page_table[(int64_t)g.req * max_pages + (g.t_begin >> 4)];

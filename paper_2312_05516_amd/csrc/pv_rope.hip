@@ -15,7 +15,7 @@
 // heads first (K rotated + scattered, V scattered as in kv_append_kernel), then the query heads of
 // the group's tokens.  The heads of a token share its angles, which are twice the bytes of one
 // head's row, so a thread loads them once for all its heads, and then all its rows at once.
-#include "pv_device.h"
+#include "pv_norm_rope.h"
 
 namespace pv {
 
@@ -173,6 +173,95 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
                                          v_pages + tile);
 }
 
+// With norms, batches of one token a request: a group of rope_append_kernel leaves all but a token's lanes
+// without work, so a wavefront of its own takes several heads of a token, 128 / (D/16) of keys or
+// queries or 512 / D of V.
+template <typename T, int D, int STYLE>
+__global__ __launch_bounds__(64) void norm_rope_step_kernel(
+    const AppendGroup *__restrict__ groups, const uint16_t *q_in,
+    uint16_t *q_out /* may be q_in */, const uint16_t *__restrict__ k_new,
+    const uint16_t *__restrict__ v_new, const float *__restrict__ cos_sin,
+    const int32_t *__restrict__ page_table, int32_t max_pages, int32_t num_q_heads,
+    int32_t num_kv_heads, uint16_t *__restrict__ k_pages, uint16_t *__restrict__ v_pages,
+    const uint16_t *__restrict__ q_weight, const uint16_t *__restrict__ k_weight, float eps)
+{
+    typedef StepHeads<D> Heads;
+    constexpr int VH = 512 / D;
+    const AppendGroup g = groups[blockIdx.x];
+    const int lane = lane_id();
+    const int k_blocks = (num_kv_heads + Heads::kHeads - 1) / Heads::kHeads;
+    const int v_blocks = (num_kv_heads + VH - 1) / VH;
+    int y = (int)blockIdx.y;
+    if (y >= k_blocks + v_blocks) {
+        const Heads mine((y - k_blocks - v_blocks) * Heads::kHeads, num_q_heads);
+        rotate_q<T, D, STYLE, 2, 1, false>(g, 0, 0, ((int64_t)g.q_row * num_q_heads + mine.first) * D,
+                                           Heads::kEach * D, mine.count, q_in, q_out, q_weight, eps,
+                                           cos_sin);
+        return;
+    }
+    const int64_t page = page_table[(int64_t)g.req * max_pages + (g.t_begin >> 4)];
+    const int slot = g.t_begin & 15;
+    const int64_t row = (int64_t)g.q_row * num_kv_heads, tile = page * num_kv_heads;
+    if (y < k_blocks) {
+        const Heads mine(y * Heads::kHeads, num_kv_heads);
+        const int c = lane % (D / 16);
+        u32x4 rows[2][2], w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int h = mine.first + (i < mine.count ? i : 0) * Heads::kEach;
+            rows[i][0] = load16(k_new + (row + h) * D + 8 * c);
+            rows[i][1] = load16(k_new + (row + h) * D + D / 2 + 8 * c);
+        }
+        ChunkAngles<D, STYLE> angle;
+        angle.load(cos_sin + (int64_t)g.t_begin * D, c);
+        if (k_weight) {
+            w[0] = load16(k_weight + 8 * c);
+            w[1] = load16(k_weight + D / 2 + 8 * c);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            norm_rotate_chunks<T, D, STYLE>(rows[i], k_weight != nullptr, w, eps, angle);
+            if (i < mine.count) {
+                uint16_t *to = k_pages + (tile + mine.first + i * Heads::kEach) * (16 * D) + slot * 8;
+                *reinterpret_cast<u32x4 *>(to + c * 128) = rows[i][0];
+                *reinterpret_cast<u32x4 *>(to + (c + D / 16) * 128) = rows[i][1];
+            }
+        }
+        return;
+    }
+    // V: lane -> head dimensions, moved bit for bit
+    const int h0 = (y - k_blocks) * VH;
+    uint16_t val[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int at = 64 * i + lane, h = min(h0 + at / D, num_kv_heads - 1);
+        val[i] = v_new[(row + h) * D + at % D];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int at = 64 * i + lane, h = h0 + at / D;
+        if (h < num_kv_heads)
+            v_pages[(tile + h) * (16 * D) + ((slot >> 3) * D + at % D) * 8 + (slot & 7)] = val[i];
+    }
+}
+
+template <typename T, int D, int STYLE>
+static void launch_norm_step_t(const pv_plan *plan, const DeviceLists &dl, const NormRope &nr,
+                               const void *k_new, const void *v_new, const int32_t *page_table,
+                               void *k_pages, void *v_pages, hipStream_t stream)
+{
+    constexpr int KH = StepHeads<D>::kHeads, VH = 512 / D;
+    const int hkv = plan->pool.num_kv_heads, hq = nr.q_in ? plan->num_q_heads : 0;
+    const dim3 grid((unsigned)plan->append_groups.size(),
+                    (unsigned)((hkv + KH - 1) / KH + (hkv + VH - 1) / VH + (hq + KH - 1) / KH));
+    hipLaunchKernelGGL((norm_rope_step_kernel<T, D, STYLE>), grid, dim3(64), 0, stream,
+                       dl.append_groups, (const uint16_t *)nr.q_in, (uint16_t *)nr.q_out,
+                       (const uint16_t *)k_new, (const uint16_t *)v_new, nr.cos_sin,
+                       page_table, plan->max_pages_per_req, plan->num_q_heads,
+                       plan->pool.num_kv_heads, (uint16_t *)k_pages, (uint16_t *)v_pages,
+                       (const uint16_t *)nr.q_weight, (const uint16_t *)nr.k_weight, nr.eps);
+}
+
 template <typename T, int D, int STYLE, int HB, bool NORM>
 static void launch_rope_t(const pv_plan *plan, const DeviceLists &dl, const NormRope &nr,
                           const void *k_new, const void *v_new, const int32_t *page_table,
@@ -196,8 +285,10 @@ static void launch_rope_t(const pv_plan *plan, const DeviceLists &dl, const Norm
 // 64/8 heads, 4 K tokens, half pairs 95 -> 91.  A small batch keeps one head a workgroup, the more of
 // them run at once (4 generation steps, 64/8 heads: 24.8 us against 25.5).
 template <typename T, int D, bool NORM>
-static auto pick_rope(int style, bool many)
+static auto pick_rope(int style, bool many, bool steps)
 {
+    if constexpr (NORM)
+        if (steps) return style == 0 ? launch_norm_step_t<T, D, 0> : launch_norm_step_t<T, D, 1>;
     if (style == 0) return many ? launch_rope_t<T, D, 0, 2, NORM> : launch_rope_t<T, D, 0, 1, NORM>;
     return many ? launch_rope_t<T, D, 1, 4, NORM> : launch_rope_t<T, D, 1, 1, NORM>;
 }
@@ -210,13 +301,14 @@ hipError_t launch_rope_append(const pv_plan *plan, const DeviceLists &dl, const 
     const bool f = plan->pool.dtype == PV_F16;
     const int64_t rows = 2 * plan->pool.num_kv_heads + (nr.q_in ? plan->num_q_heads : 0);
     const bool many = plan->total_q * rows * plan->pool.head_dim * 2 > kStreamBytes;
+    const bool steps = (int32_t)plan->append_groups.size() == plan->total_q;  // one token a group
     auto pick = [&](auto norm) {
         constexpr bool NORM = decltype(norm)::value;
         return plan->pool.head_dim == 128
-                   ? (f ? pick_rope<F16, 128, NORM>(nr.style, many)
-                        : pick_rope<BF16, 128, NORM>(nr.style, many))
-                   : (f ? pick_rope<F16, 64, NORM>(nr.style, many)
-                        : pick_rope<BF16, 64, NORM>(nr.style, many));
+                   ? (f ? pick_rope<F16, 128, NORM>(nr.style, many, steps)
+                        : pick_rope<BF16, 128, NORM>(nr.style, many, steps))
+                   : (f ? pick_rope<F16, 64, NORM>(nr.style, many, steps)
+                        : pick_rope<BF16, 64, NORM>(nr.style, many, steps));
     };
     auto go = nr.q_weight || nr.k_weight ? pick(std::true_type{}) : pick(std::false_type{});
     go(plan, dl, nr, k_new, v_new, page_table, k_pages, v_pages, stream);

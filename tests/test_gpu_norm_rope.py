@@ -94,6 +94,32 @@ def test_norm_and_rotation_into_16_bit_pools(heads, dtype, style):
 
 
 @pytest.mark.parametrize("style", ["interleaved", "half"])
+@pytest.mark.parametrize("heads,dtype", [((64, 8, 128), "bf16"), ((40, 40, 128), "f16"), ((17, 17, 64), "bf16"),
+                                         ((33, 33, 64), "f16"), ((7, 1, 128), "f16"), ((9, 3, 64), "bf16")])
+def test_one_token_to_every_request(heads, dtype, style):
+    """Every slot of a page, a token that ends one page and one that begins the next; heads that do not
+    fill the last wavefront; either weight, or both."""
+    ctx = tuple(range(18)) + (31, 32, 700)
+    for new in ((1,) * 21, (0, 2) + (1,) * 13 + (2,) + (0,) * 5):  # positions 15 and 16 of one request
+        b = _batch(heads, dtype, ctx, new)
+        q, k, v, w = _inputs(b, 6)
+        q_out, k_rows, v_rows, (kb, vb) = _call16(b, q, k, v, w, style)
+        _close(q_out, q, w[0], b, style)
+        _close(k_rows, k, w[1], b, style)
+        assert np.array_equal(v_rows, v)
+        nan = wl.nan_pattern(dtype)
+        assert (kb == nan).sum() == (vb == nan).sum() == kb.size - k.size
+        again = _call16(b, q, k, v, w, style, in_place=True)
+        assert np.array_equal(again[0], q_out) and np.array_equal(again[3][0], kb)
+        q_out, k_rows, v_rows, _ = _call16(b, q, k, v, (w[0], None), style)
+        _close(q_out, q, w[0], b, style)
+        _close(k_rows, k, None, b, style)
+        _, k_rows, v_rows, (kb, vb) = _call16(b, None, k, v, (None, w[1]), style)
+        _close(k_rows, k, w[1], b, style)
+        assert np.array_equal(v_rows, v) and (kb == nan).sum() == kb.size - k.size
+
+
+@pytest.mark.parametrize("style", ["interleaved", "half"])
 @pytest.mark.parametrize("heads,dtype", [((70, 7, 128), "bf16"), ((33, 11, 64), "f16")])
 def test_many_rows(heads, dtype, style):
     """Batches over 32 MiB of rows take several heads a workgroup."""
