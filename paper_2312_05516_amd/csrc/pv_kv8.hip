@@ -18,7 +18,7 @@
 //
 // Measured: 8 prompts, 6.5 K tokens, 40 KV heads, 201 MB in 38.2 us = 5.25 TB/s (a device copy of 1 GiB:
 // 5.2); reading 70 K tokens of 8 heads back, 427 MB in 85.1 us = 5.0 TB/s; norms and rotation in front, 4.4 K
-// tokens, 64/8 heads, 172 MB in 33.7 us = 5.1 TB/s; 256 generation steps 4.2 us, launch and latency.
+// tokens, 64/8 heads, 172 MB in 33.7 us = 5.1 TB/s; 256 generation steps 3.6 us, launch and latency.
 #include "pv_kv8.h"
 #include "pv_norm_rope.h"
 
@@ -315,8 +315,11 @@ __global__ __launch_bounds__(128) void kv8_append_kernel(
 
 // Batches that bring one token a request.  Whole pages a wavefront would leave most lanes without work,
 // so a wavefront of its own takes several heads of one token: the K rows of 128 / (D / 16) heads (lane =
-// head and the 32 dimensions of append_k8), V of a quarter as many (lane = 8 dimensions), or the
-// queries of as many heads as K.  A page that has to be rounded anew is the whole wavefront's work.
+// head and the 32 dimensions of append_k8), V of two, or the queries of as many heads as K.  A page that has
+// to be rounded anew is the whole wavefront's work.  V's codes lie 16 bytes apart, a line for eight of them:
+// with neighbouring lanes on neighbouring dimensions 256 requests, 40 heads take 8.6 us (12.2 with 8
+// dimensions a lane), 8 heads 3.6 (4.4); four heads of V a wavefront 8.5 and 3.75, 32 requests 2.83 (2.66).
+constexpr int kStepHeadsV = 2;
 template <typename T, int D, int STYLE>
 __global__ __launch_bounds__(64) void kv8_step_kernel(
     const AppendGroup *__restrict__ groups, const uint16_t *q_in, uint16_t *q_out /* may be q_in */,
@@ -326,7 +329,7 @@ __global__ __launch_bounds__(64) void kv8_step_kernel(
     int32_t num_q_heads, int32_t num_kv_heads, Kv8Ptrs pool)
 {
     constexpr int LPT = D / 32, KH = 64 / LPT;  // lanes a head and heads, of K and queries
-    constexpr int VL = D / 8, VH = 64 / VL;     // the same of V
+    constexpr int VH = kStepHeadsV;             // heads of V
     const AppendGroup g = groups[blockIdx.x];
     const int lane = lane_id();
     const int k_blocks = (num_kv_heads + KH - 1) / KH, v_blocks = (num_kv_heads + VH - 1) / VH;
@@ -387,35 +390,55 @@ __global__ __launch_bounds__(64) void kv8_step_kernel(
         return;
     }
     y -= k_blocks;
-    const int u = lane / VL, c = lane % VL;
-    const bool valid = y * VH + u < num_kv_heads;
-    const int h = valid ? y * VH + u : num_kv_heads - 1;
-    const int64_t tile = page * num_kv_heads + h;
-    u32x4 raw = load16(v_new + ((int64_t)g.q_row * num_kv_heads + h) * D + 8 * c);
-    const int before = s0 > 0 ? (int)pool.v_scales[tile] - 127 : kNoExponent;
-    uint32_t mag = 0;
+    // V: a lane holds dimensions lane, lane + 64, .. of the heads one behind the other, so that its codes lie
+    // 16 bytes from its neighbours'.  values[i / 2] holds the i-th; the heads' exponents are the wavefront's.
+    const int h0 = y * VH, heads = min(VH, num_kv_heads - h0);
+    constexpr int EACH = D / 64, N = VH * EACH;  // values of a head, and of all
+    const int64_t tile = page * num_kv_heads + h0;
+    const int scales = pool.v_scales[tile + min(lane, heads - 1)];  // of a page that is begun: not used
+    uint32_t values[N / 2];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mag = max_magnitudes(mag, finite_magnitudes<T>(raw[w]));
-    mag = max_of_lanes<VL>(mag);
-    const int e = max(needed_exponent<T>(max(mag & 0xFFFFu, mag >> 16)), before);
-    if (__any(e == Kv8<T>::kMaxExp)) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) raw[w] = e == Kv8<T>::kMaxExp ? limit_to_top<T>(raw[w]) : raw[w];
+    for (int i = 0; i < N; ++i) {
+        const int h = h0 + (i / EACH < heads ? i / EACH : 0);
+        const uint32_t x = v_new[((int64_t)g.q_row * num_kv_heads + h) * D + i % EACH * 64 + lane];
+        values[i / 2] = i % 2 ? values[i / 2] | x << 16 : x;
     }
-    uint64_t grown = s0 > 0 ? __ballot(valid && c == 0 && e > before) : 0;
+    int before[VH], e[VH];
+#pragma unroll
+    for (int i = 0; i < VH; ++i)
+        before[i] = s0 > 0 ? __builtin_amdgcn_readlane(scales, i) - 127 : kNoExponent;
+    uint32_t mags[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) mags[i] = finite_magnitudes<T>(values[i]);
+#pragma unroll
+    for (int i = 0; i < VH; i += 2) {  // two heads' magnitudes side by side
+        uint32_t two = mags[i / 2];  // EACH == 1: values hold them so
+        if constexpr (EACH == 2) {
+            const uint32_t a = mags[i], b = mags[i + 1];
+            two = (max_magnitudes(a, a >> 16) & 0xFFFFu) | (max_magnitudes(b, b << 16) & 0xFFFF0000u);
+        }
+        two = __builtin_amdgcn_readfirstlane(max_of_lanes<64>(two));
+        e[i] = max(needed_exponent<T>(two & 0xFFFFu), before[i]);
+        e[i + 1] = max(needed_exponent<T>(two >> 16), before[i + 1]);
+    }
+    bool grown = false;
+#pragma unroll
+    for (int i = 0; i < VH; ++i) grown |= i < heads && s0 > 0 && e[i] > before[i];
     if (grown) {
-        for (; grown; grown &= grown - 1) {
-            const int from = __ffsll((long long)grown) - 1;
-            const int b = __builtin_amdgcn_readlane(before, from);
-            const int a = __builtin_amdgcn_readlane(e, from);
-            uint8_t *at = pool.v + (page * num_kv_heads + y * VH + from / VL) * (16 * D);
+#pragma unroll 1
+        for (int i = 0; i < heads; ++i) {
+            const int from = __builtin_amdgcn_readlane(scales, i) - 127;
+            int to = e[0];
+#pragma unroll
+            for (int k = 1; k < VH; ++k) to = i == k ? e[k] : to;
+            if (to <= from) continue;
             for (int d = lane; d < D; d += 64) {
-                u32x4 *p = reinterpret_cast<u32x4 *>(at + d * 16);
+                u32x4 *p = reinterpret_cast<u32x4 *>(pool.v + (tile + i) * (16 * D) + d * 16);
                 u32x4 codes = *p;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const uint32_t front = codes_in_front(s0 - 4 * w);
-                    codes[w] = (rescale4(codes[w], b, a) & front) | (codes[w] & ~front);
+                    codes[w] = (rescale4(codes[w], from, to) & front) | (codes[w] & ~front);
                 }
                 *p = codes;
             }
@@ -423,16 +446,17 @@ __global__ __launch_bounds__(64) void kv8_step_kernel(
         __builtin_amdgcn_s_waitcnt(0);  // the new token's codes, below, lie among these bytes
         asm volatile("" ::: "memory");
     }
-    if (valid) {
-        uint8_t *at = pool.v + tile * (16 * D) + c * 128 + s0;
-        const float scale = exp2_scale(e + 127);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const uint32_t two = Kv8<T>::template encode2<false>(0u, raw[w], scale);
-            at[32 * w] = (uint8_t)two;
-            at[32 * w + 16] = (uint8_t)(two >> 8);
-        }
-        if (c == 0 && e != before) pool.v_scales[tile] = (uint8_t)(e + 127);
+    for (int i = 0; i < VH; ++i) {
+        if (i >= heads) break;
+        const float scale = exp2_scale(e[i] + 127);
+        uint32_t xy = EACH == 2 ? values[i] : i % 2 ? values[i / 2] >> 16 : values[i / 2] & 0xFFFFu;
+        if (e[i] == Kv8<T>::kMaxExp) xy = limit_to_top<T>(xy);
+        const uint32_t codes = Kv8<T>::template encode2<false>(0u, xy, scale);
+        uint8_t *at = pool.v + (tile + i) * (16 * D) + lane * 16 + s0;
+        at[0] = (uint8_t)codes;
+        if constexpr (EACH == 2) at[64 * 16] = (uint8_t)(codes >> 8);
+        if (lane == 0 && e[i] != before[i]) pool.v_scales[tile + i] = (uint8_t)(e[i] + 127);
     }
 }
 
@@ -526,8 +550,8 @@ __global__ __launch_bounds__(128) void kv8_read_kernel(
 }
 
 // Rules, us a call (three batches in turn, so that small ones find their rows in a cache):
-//  * Batches of one token a request take the kernel for them: 256 requests, 8 KV heads 4.5 (5.5 with the
-//    kernel for pages), 40 heads 12.2 (15.7).
+//  * Batches of one token a request take the kernel for them: 256 requests, 8 KV heads 3.6 (5.5 with the
+//    kernel for pages), 40 heads 8.6 (15.7).
 //  * With rotation more than 32 MiB of rows take two heads a wavefront, which share the angles: 6
 //    prompts, 40/40 heads, 4.8 K tokens 53.3 (one: 56.0), 8 of 300, 64/8 heads 21.1 (22.8), but 2 of 100
 //    5.6 (4.3).  Without rotation one head is ahead (6 K tokens, 40 heads: 39.7, two 41.4).
@@ -547,7 +571,7 @@ static void launch_append8_t(const pv_plan *plan, const DeviceLists &dl, const N
     const bool two = STYLE >= 0 && row_bytes > kStreamBytes;
     const bool streams = STYLE < 0 ? row_bytes > 2 * kStreamBytes
                                    : D == 128 && 2 * row_bytes > 3 * kStreamBytes;
-    constexpr int KH = 64 / (D / 32), VH = 64 / (D / 8);
+    constexpr int KH = 64 / (D / 32), VH = kStepHeadsV;
     const int heads = (two ? 2 : 1) * (128 / D);
     const int blocks = steps ? (hkv + KH - 1) / KH + (hkv + VH - 1) / VH + (hq + KH - 1) / KH
                              : (hkv + heads - 1) / heads + (hq + 2 * heads - 1) / (2 * heads);

@@ -20,7 +20,8 @@
 namespace pv {
 
 // NORM: rows whose kind has a weight are first scaled to y = x * w / sqrt(mean(x^2) + eps), in fp32
-// and without a rounding of their own; the lanes that hold a row are neighbours.
+// and without a rounding of their own; the lanes that hold a row are neighbours.  Bound: HBM, as without.
+// 6 prompts, 4.8 K tokens, 40/40 heads: 296 MB in 63 us = 4.7 TB/s.
 template <typename T, int D, int STYLE, int HB, bool NORM>
 __global__ __launch_bounds__(D) void rope_append_kernel(
     const AppendGroup *__restrict__ groups, const uint16_t *q_in,
@@ -175,7 +176,8 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
 
 // With norms, batches of one token a request: a group of rope_append_kernel leaves all but a token's lanes
 // without work, so a wavefront of its own takes several heads of a token, 128 / (D/16) of keys or
-// queries or 512 / D of V.
+// queries or 512 / D of V.  64 requests, 64/8 heads 3.0 us (4.4 in rope_append_kernel), 256 requests, 40/40
+// heads 10.1 (13.9): 16 MB of rows, but a token's V is 2 of every 16 bytes of 21 MB.
 template <typename T, int D, int STYLE>
 __global__ __launch_bounds__(64) void norm_rope_step_kernel(
     const AppendGroup *__restrict__ groups, const uint16_t *q_in,
