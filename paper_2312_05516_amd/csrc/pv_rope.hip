@@ -21,7 +21,14 @@ namespace pv {
 
 // NORM: rows whose kind has a weight are first scaled to y = x * w / sqrt(mean(x^2) + eps), in fp32
 // and without a rounding of their own; the lanes that hold a row are neighbours.  Bound: HBM, as without.
-// 6 prompts, 4.8 K tokens, 40/40 heads: 296 MB in 63 us = 4.7 TB/s.
+// 6 prompts, 4.8 K tokens, 40/40 heads: 296 MB in 62 us = 4.8 TB/s (between calls).
+//
+// kVApart: V in workgroups of its own, in front of the others.  Behind K's norms and rotation its loads come
+// late: the same 6 prompts 65.2 us otherwise, 63.0 so (half pairs 62.4 and 61.6, 64/8 heads the same; head
+// size 64 1-2 % slower).
+template <int D, int HB, bool NORM>
+constexpr bool kVApart = NORM && HB > 1 && D == 128;
+
 template <typename T, int D, int STYLE, int HB, bool NORM>
 __global__ __launch_bounds__(D) void rope_append_kernel(
     const AppendGroup *__restrict__ groups, const uint16_t *q_in,
@@ -34,7 +41,9 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
     constexpr int CH = D / 8;
     const AppendGroup g = groups[blockIdx.x];
     const int kv_blocks = (num_kv_heads + HB - 1) / HB;
-    const int y = (int)blockIdx.y;
+    constexpr bool V_APART = kVApart<D, HB, NORM>;
+    const bool v_only = V_APART && (int)blockIdx.y < kv_blocks;
+    const int y = (int)blockIdx.y - (V_APART && !v_only ? kv_blocks : 0);
     const int t = (int)threadIdx.x;
     const bool is_q = y >= kv_blocks;
     const int h0 = (is_q ? y - kv_blocks : y) * HB;
@@ -68,7 +77,9 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
                 val;
     };
 
-    if constexpr (STYLE == 0) {
+    if (v_only) {
+        // below
+    } else if constexpr (STYLE == 0) {
         // one thread per (token j, chunk c8): 4 pairs inside the chunk, of every head
         const int j = t / CH, c8 = t % CH;
         if (j < g.count) {
@@ -169,7 +180,7 @@ __global__ __launch_bounds__(D) void rope_append_kernel(
     }
 
     // V: thread -> head dimension d = t, moved bit for bit
-    if (!is_q)
+    if (V_APART ? v_only : !is_q)
         scatter_v_group<D, HB, (HB > 1)>(v_new + src_off, row_stride, g.count, heads, slot0, t,
                                          v_pages + tile);
 }
@@ -271,7 +282,8 @@ static void launch_rope_t(const pv_plan *plan, const DeviceLists &dl, const Norm
 {
     const int kv_blocks = (plan->pool.num_kv_heads + HB - 1) / HB;
     const int q_blocks = nr.q_in ? (plan->num_q_heads + HB - 1) / HB : 0;
-    const dim3 grid((unsigned)plan->append_groups.size(), (unsigned)(kv_blocks + q_blocks));
+    const int v_blocks = kVApart<D, HB, NORM> ? kv_blocks : 0;
+    const dim3 grid((unsigned)plan->append_groups.size(), (unsigned)(v_blocks + kv_blocks + q_blocks));
     hipLaunchKernelGGL((rope_append_kernel<T, D, STYLE, HB, NORM>), grid, dim3(D), 0, stream,
                        dl.append_groups, (const uint16_t *)nr.q_in, (uint16_t *)nr.q_out,
                        (const uint16_t *)k_new, (const uint16_t *)v_new, nr.cos_sin,
