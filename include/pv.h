@@ -171,8 +171,9 @@ pv_status pv_plan_work_item(const pv_plan *plan, int32_t kind, int32_t index, in
  * bandwidth-oriented kernel takes its probabilities in two 16-bit terms, 2 = it reads K/V with the
  * streaming hint, 4 = items of the matrix-core kernel (128 rows) renew their reference maximum, 8 =
  * items of it that alone read their K/V do so with the streaming hint (the kernel still excepts pages
- * that requests share), 16 = the 256-row kernel applies the scale to the scores, not the queries (over 8-bit pools these
- * kernels have 2 and 16 always and no other variant).  -1 for NULL. */
+ * that requests share), 16 = the 256-row kernel applies the scale to the scores, not the queries, 32 = an item of the
+ * bandwidth-oriented kernel has eight wavefronts, not four.  (Over 8-bit pools the kernels have 2 and 16 always
+ * and none of 1, 4 and 8; over 16-bit pools not 32.)  -1 for NULL. */
 int32_t pv_plan_kernel_variants(const pv_plan *plan);
 
 /* Host-side check of a page table against the plan (host copy of the table, row stride

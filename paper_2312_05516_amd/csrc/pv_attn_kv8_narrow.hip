@@ -5,8 +5,9 @@
 // nothing is rounded by that: the result is that of 16-bit attention over the values that reading the
 // pools back would give.
 //
-// Mapping to gfx950.  One workgroup = 4 wavefronts = one item; the wavefronts take the 64-key blocks
-// (four pages) of the item round-robin, two blocks' loads in flight, nothing is shared until the end.
+// Mapping to gfx950.  One workgroup = 4 wavefronts (8 in short lists, see pv_plan::narrow_eight) = one
+// item; the wavefronts take the 64-key blocks (four pages) of the item round-robin, two blocks' loads in
+// flight, nothing is shared until the end.
 // A lane's 16 bytes are 16 codes: of K 16 dimensions of one slot, two operands of
 // v_mfma_f32_16x16x32 (S^T = K Q^T, the dimensions contracted in that order); of V the 16 slots of
 // one dimension.  S^T row 4g + i of the b-th of a block's four score tiles is fed with slot 4b + i of
@@ -30,14 +31,13 @@ struct Narrow8Frag {
     uint32_t k_scale, v_scale;
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attn_kv8_narrow_kernel(
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_kv8_narrow_kernel(
     const WorkItem *__restrict__ items, const uint16_t *__restrict__ q, Kv8Ptrs pool,
     const int32_t *__restrict__ page_table, int32_t max_pages, int32_t num_q_heads,
     int32_t num_kv_heads, int32_t group, float scale_log2e, uint16_t *__restrict__ out,
     float *__restrict__ ws_o, float *__restrict__ ws_ml)
 {
-    constexpr int NW = 4;
     constexpr int BK = 64;
     constexpr int JJ = D / 64;
     constexpr int NB = D / 16;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256, 2) void attn_kv8_narrow_kernel(
             }
         }
     }
-    finish_narrow_item<T, D>(it, group, num_q_heads, o, m_run, l_run, sm_o, sm_m, sm_l, out, ws_o,
+    finish_narrow_item<T, D, NW>(it, group, num_q_heads, o, m_run, l_run, sm_o, sm_m, sm_l, out, ws_o,
                              ws_ml);
 }
 
@@ -241,8 +241,9 @@ static void launch_kv8_narrow_t(const pv_plan *plan, const DeviceLists &dl, cons
                                 const Kv8Ptrs &pool, const int32_t *page_table, float scale,
                                 void *out, float *ws_o, float *ws_ml, hipStream_t stream)
 {
-    hipLaunchKernelGGL((attn_kv8_narrow_kernel<T, D>), dim3((unsigned)plan->narrow.size()), dim3(256), 0,
-                       stream, dl.narrow, (const uint16_t *)q, pool, page_table, plan->max_pages_per_req,
+    auto kernel = plan->narrow_eight ? attn_kv8_narrow_kernel<T, D, 8> : attn_kv8_narrow_kernel<T, D, 4>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)plan->narrow.size()),
+                       dim3(plan->narrow_eight ? 512 : 256), 0, stream, dl.narrow, (const uint16_t *)q, pool, page_table, plan->max_pages_per_req,
                        plan->num_q_heads, plan->pool.num_kv_heads, plan->group, scale * kLog2e,
                        (uint16_t *)out, ws_o, ws_ml);
 }

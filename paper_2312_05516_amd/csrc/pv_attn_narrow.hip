@@ -239,7 +239,7 @@ __global__ __launch_bounds__(256, 2) void attn_narrow_kernel(
 
     if constexpr (AHEAD) asm volatile("" ::"v"(touched));
 
-    finish_narrow_item<T, D>(it, group, num_q_heads, o, m_run, l_run, sm_o, sm_m, sm_l, out, ws_o,
+    finish_narrow_item<T, D, NW>(it, group, num_q_heads, o, m_run, l_run, sm_o, sm_m, sm_l, out, ws_o,
                              ws_ml);
 }
 

@@ -775,8 +775,10 @@ pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_
     // Over 8-bit pools the narrow kernel takes half the time for a key (one item over 30 K keys 6.3 ns, 3.7
     // with head size 64) and steps of 64 keys.  Counted with 16 ns, attention call: 32 generation steps
     // over 2 K, 64/8 heads, 33.8 us in 512 parts (30.1 whole), 16 of 0.5-4 K, 40/40 heads, 78.2 with the
-    // longest cut (73.6 whole).
-    const int32_t narrow_ns = kv8         ? (wide_rows ? 5 : 4)
+    // longest cut (73.6 whole).  Up to half as many items as CUs wait for their own loads: 7 ns.  64/8 heads,
+    // one request of 1500 keys 8.3 us cut (12.5 with 5 ns, whole), 2 8.7 (11.0), 4 of 200-2000 10.7 (14.8); 20 of
+    // 200-1800 15.9 cut (15.5 whole), 48 of 200-2000 30.1 (27.7), so no more than those.
+    const int32_t narrow_ns = kv8         ? (!wide_rows ? 4 : (int64_t)plan->narrow.size() <= kCUs / 2 ? 7 : 5)
                               : wide_rows ? 16
                                           : (int64_t)plan->narrow.size() > kNarrowSlots ? 12 : 9;
     const CutRule narrow_rule = {
@@ -792,6 +794,9 @@ pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_
     // in 16-bit results 1.3 to 1.4 times as far as those' own rounding; two terms would take 6 % of the
     // time of a list that does not fill the GPU (16 steps over 900 keys, 64/8 heads 13.6 us, 12.8 without).
     if (kv8) plan->narrow_two_terms = plan->wide_renews = false;
+    plan->narrow_eight = false;
+    if (kv8 && plan->narrow.size() <= (size_t)kCUs)
+        for (const WorkItem &w : plan->narrow) plan->narrow_eight |= item_cost(w) > 4 * 64;
     plan->wide_streams = kv_bytes > kStreamKvBytes && wide_once * 3 >= wide_shared;
     plan->narrow_streams = narrow_once > narrow_shared * 4;
     const bool by_time = kv8 && !tune.split_by_hand && !plan->tile256.empty();
@@ -967,7 +972,9 @@ int32_t pv_plan_num_work_items(const pv_plan *plan, int32_t kind)
 int32_t pv_plan_kernel_variants(const pv_plan *plan)
 {
     if (!plan) return -1;
-    if (plan->kv8) return (plan->narrow.empty() ? 0 : 2) | (plan->tile256.empty() ? 0 : 16);
+    if (plan->kv8)
+        return (plan->narrow.empty() ? 0 : 2) | (plan->tile256.empty() ? 0 : 16) |
+               (plan->narrow_eight ? 32 : 0);
     return (plan->narrow_two_terms ? 1 : 0) | (plan->narrow_streams ? 2 : 0) |
            (plan->wide_renews ? 4 : 0) | (plan->wide_streams ? 8 : 0) |
            (plan->tile_scales_scores ? 16 : 0);

@@ -269,6 +269,12 @@ struct pv_plan {
     // K/V with the streaming hint: items of the 128-row kernel that are `alone` and share no pages;
     // all of the narrow kernel's
     bool wide_streams, narrow_streams;
+    // 8-bit pools: eight wavefronts an item instead of four.  A CU has room for eight of this kernel, which
+    // one item of four leaves half empty where there are no more items than CUs; items of four blocks
+    // or less have no use for more.  Attention call, us with eight (four), 64/8 heads: one request of 60
+    // keys 4.5 (4.2), 300 5.6 (5.6), 700 6.6 (7.1), 1500 12.6 (14.5); 16 of 300-1500 13.4 (15.2), 30 of 100-1000
+    // 11.6 (12.4); head size 64, 32/8 heads: 700 5.0 (5.7), 32 of 900-1100 9.6 (10.4).
+    bool narrow_eight;
     // 256-row kernel: no scaled queries (see kTileMinItems)
     bool tile_scales_scores;
     size_t workspace_bytes;

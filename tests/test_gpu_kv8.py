@@ -193,6 +193,17 @@ def test_generation_steps(heads, dtype):
 
 
 @pytest.mark.parametrize("heads,dtype", GROUPS)
+def test_generation_steps_of_many_requests(heads, dtype):
+    """More items than CUs have four wavefronts each, fewer have eight."""
+    ctx = [0, 1, 14, 15, 16, 62, 63, 64, 127, 255, 256, 300, 511, 700]
+    ctx = ctx * (257 // (len(ctx) * heads[1]) + 1)
+    b = _batch(ctx, [1] * len(ctx), heads, dtype)
+    run = R.Run(b)
+    assert run.pv.plan_kernel_variants(run.plan) == 2
+    _check_attention(b, *R.filled(b, 102))
+
+
+@pytest.mark.parametrize("heads,dtype", GROUPS)
 def test_prompts(heads, dtype):
     b = _batch([0, 0, 5, 130, 64, 33, 1], [1, 17, 33, 70, 200, 0, 129], heads, dtype)
     _check_attention(b, *R.filled(b, 110))

@@ -69,8 +69,10 @@ def test_plans_for_8_bit_pools():
     for ctx, new, kind in (((20000,) * 8, (512,) * 8, 3), ((900, 300), (100, 90), 1), ((900, 300), (1, 1), 0)):
         q = _plan(ctx=ctx, new=new, heads=(64, 8, 128), max_pages=2000, pages=20000)
         assert [pv.plan_num_work_items(q, k) > 0 for k in (0, 1, 3)] == [kind == k for k in (0, 1, 3)]
-        variants = pv.plan_kernel_variants(q)  # of those kernels the only ones there are
-        assert variants == {0: 2, 1: 0, 3: 16}[kind]
+        assert pv.plan_kernel_variants(q) == {0: 2 + 32, 1: 0, 3: 16}[kind]
+    for ctx, variants in (((900,) * 33, 2), ((900,) * 32, 2 + 32), ((250,) * 32, 2), ((250, 256), 2 + 32)):
+        q = _plan(ctx=ctx, new=(1,) * len(ctx), heads=(64, 8, 128), max_pages=60, pages=2000)
+        assert pv.plan_kernel_variants(q) == variants
     for bad, status in (((pv.pool_desc(4, 2, 96, "f16"), 4, [1], [1], 4), UNSUPPORTED),
                         ((pv.pool_desc(4, 2, 64, "f16"), 3, [1], [1], 4), INVALID),
                         ((pv.pool_desc(4, 2, 64, "f16"), 4, [-1], [1], 4), INVALID),
