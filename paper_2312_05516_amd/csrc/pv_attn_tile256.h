@@ -46,7 +46,7 @@
 // have put them (four stages of it suffice: block b + 3 is written while b to b + 2 are read).  So a
 // code is widened once for 256 rows, 16 conversions and 4 stores for a thread's 32 matrix-core
 // instructions.  Scores are always scaled in fp32.  512 new tokens each over 19-25 K keys, 4 requests, 64/8
-// heads: 1433 GFLOP in 1164-1226 us = 1.17-1.23 PFLOP/s (a library bf16 product of 8192^3: 1.27).
+// heads: 1433 GFLOP in 1164-1255 us = 1.14-1.23 PFLOP/s (a library bf16 product of 8192^3: 1.27).
 #pragma once
 
 #include <type_traits>
