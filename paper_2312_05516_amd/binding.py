@@ -408,12 +408,21 @@ def norm_rope_kv_append_planned(plan: Plan, q_in, q_out, k_new, v_new, q_weight,
 
 class Kv8Pool:
     """The four device arrays of an 8-bit K/V pool (kept alive): codes of K and V, of
-    kv8_pool_bytes(desc) bytes each, and their scales, of kv8_scale_bytes(desc) bytes each."""
+    kv8_pool_bytes(desc) bytes each, and their scales, of kv8_scale_bytes(desc) bytes each.  A call
+    takes their addresses when it is made, so an array may be replaced, or given another storage."""
 
     def __init__(self, k, v, k_scales, v_scales):
         self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
-        self._ptrs = _Kv8Ptrs(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales))
-        self._ref = ctypes.byref(self._ptrs)
+        self._held = (None, None)
+        self._ref  # refuses what has no address
+
+    @property
+    def _ref(self):
+        at = _ptr(self.k), _ptr(self.v), _ptr(self.k_scales), _ptr(self.v_scales)
+        held = self._held
+        if held[0] != at:  # a struct of its own: a call of another thread may be reading the other
+            self._held = held = (at, ctypes.byref(_Kv8Ptrs(*at)))
+        return held[1]
 
 
 def kv8_pool_bytes(desc: PoolDesc) -> int:
