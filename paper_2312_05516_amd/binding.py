@@ -413,15 +413,24 @@ class Kv8Pool:
 
     def __init__(self, k, v, k_scales, v_scales):
         self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
-        self._held = (None, None)
         self._ref  # refuses what has no address
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_held", (None, None))
 
     @property
     def _ref(self):
-        at = _ptr(self.k), _ptr(self.v), _ptr(self.k_scales), _ptr(self.v_scales)
+        try:
+            at = (self.k.data_ptr(), self.v.data_ptr(), self.k_scales.data_ptr(),
+                  self.v_scales.data_ptr())
+        except AttributeError:  # not all of them are tensors
+            at = 0
         held = self._held
-        if held[0] != at:  # a struct of its own: a call of another thread may be reading the other
-            self._held = held = (at, ctypes.byref(_Kv8Ptrs(*at)))
+        if not at or held[0] != at:  # arrays that were not looked at yet
+            held = at, ctypes.byref(_Kv8Ptrs(_ptr(self.k), _ptr(self.v), _ptr(self.k_scales),
+                                             _ptr(self.v_scales)))
+            object.__setattr__(self, "_held", held)
         return held[1]
 
 

@@ -61,3 +61,27 @@ def test_addresses_are_those_of_the_call(monkeypatch, name):
     setattr(pool, name, torch.zeros(8, 2, dtype=torch.uint8)[:, 0])
     with pytest.raises(ValueError):
         run(pool)
+
+
+def test_strided_views_of_the_same_address_are_refused(monkeypatch):
+    run = _calls(monkeypatch)
+    arrays = {n: torch.zeros(64, dtype=torch.uint8) for n in ("k", "v", "k_scales", "v_scales")}
+    pool = pv.Kv8Pool(**arrays)
+    run(pool)
+    pool.v = arrays["v"][::2]
+    with pytest.raises(ValueError):
+        run(pool)
+    pool.v = arrays["v"]
+    assert run(pool) == tuple(a.data_ptr() for a in arrays.values())
+
+
+def test_addresses_as_numbers_and_arrays(monkeypatch):
+    import numpy as np
+    run = _calls(monkeypatch)
+    n = np.zeros(64, np.uint8)
+    pool = pv.Kv8Pool(4096, n, 8192, torch.zeros(4))
+    assert run(pool) == (4096, n.ctypes.data, 8192, pool.v_scales.data_ptr())
+    pool.k = 12288
+    assert run(pool)[0] == 12288
+    with pytest.raises(TypeError):
+        pv.Kv8Pool("k", n, n, n)
