@@ -378,8 +378,9 @@ pv_status pv_norm_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *
  * in no other request with new tokens in that page (one page has one scale, which one writer sets).  A
  * request that only reads such a page sees its earlier codes as the writer leaves them.
  *
- * Pools of head size 128 can be swapped out by pv_pages_gather and pv_pages_scatter under a description
- * with head_dim 64, whose 16-bit pages have the same bytes; the caller moves the scales.
+ * Pages can be swapped out by pv_pages_gather and pv_pages_scatter under the description of a 16-bit pool
+ * whose pages have the same bytes: head_dim 64 for head size 128, head_dim 64 and half the KV heads for head
+ * size 64 and an even number of them (for an odd one there is none); the caller moves the scales.
  */
 typedef struct {
     void *k, *v;                  /* device, 16-byte aligned */
