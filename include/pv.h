@@ -172,8 +172,9 @@ pv_status pv_plan_work_item(const pv_plan *plan, int32_t kind, int32_t index, in
  * streaming hint, 4 = items of the matrix-core kernel (128 rows) renew their reference maximum, 8 =
  * items of it that alone read their K/V do so with the streaming hint (the kernel still excepts pages
  * that requests share), 16 = the 256-row kernel applies the scale to the scores, not the queries, 32 = an item of the
- * bandwidth-oriented kernel has eight wavefronts, not four.  (Over 8-bit pools the kernels have 2 and 16 always
- * and none of 1, 4 and 8; over 16-bit pools not 32.)  -1 for NULL. */
+ * bandwidth-oriented kernel has eight wavefronts, not four.  (Over 8-bit pools the bandwidth-oriented kernel always
+ * has 2 and the 256-row kernel 16, which the sum holds where the plan has items of that kernel, and none has 1, 4
+ * or 8; over 16-bit pools there is no 32.)  -1 for NULL. */
 int32_t pv_plan_kernel_variants(const pv_plan *plan);
 
 /* Host-side check of a page table against the plan (host copy of the table, row stride
@@ -347,7 +348,10 @@ pv_status pv_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *q_out
  *   q_weight, k_weight : device [D] of the pool's type, 16-byte aligned, shared by all heads; NULL =
  *                        rows of that kind are not normalised, only rotated
  *   eps                : finite and positive, else PV_ERR_INVALID_ARG (a row of zeros stays zero)
- * Everything else as for pv_rope_kv_append_planned.  One launch, asynchronous, no allocation.
+ * Everything else as for pv_rope_kv_append_planned.  One launch, asynchronous, no allocation.  With neither
+ * weight the results are that call's, bit for bit; beside a kind with a weight, one without may differ from
+ * it by one 16-bit step (and by the last bit of the terms of the rotation), since either fuses other
+ * multiplications with the additions behind them.
  */
 pv_status pv_norm_rope_kv_append_planned(pv_plan *plan, const void *q_in, void *q_out,
                                          const void *k_new, const void *v_new,
@@ -410,9 +414,9 @@ int32_t pv_plan_is_kv8(const pv_plan *plan);
  * that is more than it was, the codes of the slots in front of the first new token become
  * round(code * 2^(old e - e)).  New codes are round(x / 2^e); with the largest e, finite values are
  * limited to 240 * 2^e first (256 * 2^e is past the 16-bit type).  Infinities and NaN become NaN.
- * round: to the nearest code, ties to even.  The result is unique, bit for bit.  Codes of other
- * slots, those behind the new tokens among them, keep their bits (not their meaning, if the
- * scale changes).
+ * round: to the nearest code, ties to even.  The result is unique, bit for bit, but for the sign of zeros
+ * and NaNs, which is not defined.  Codes of other slots, those behind the new tokens among them, keep their
+ * bits (not their meaning, if the scale changes).
  *   k_new, v_new : device [total_q, Hkv, D], 16-byte aligned
  * One launch, asynchronous, no allocation.
  */
@@ -420,8 +424,11 @@ pv_status pv_kv8_append_planned(pv_plan *plan, const void *k_new, const void *v_
                                 const int32_t *page_table, const pv_kv8_pool *pool, void *stream);
 
 /* pv_norm_rope_kv_append_planned into 8-bit pools: queries and keys are rotated (and normalised, where
- * a weight is given) and rounded to 16 bits as there, and keys and values then go through
- * pv_kv8_append_planned, in one launch. */
+ * a weight is given) and rounded to 16 bits by the same formula, and keys and values then go through
+ * pv_kv8_append_planned, in one launch.  The 16-bit values are the other call's bit for bit in bf16 with
+ * both weights.  In f16, or with fewer weights, a few may differ by one 16-bit step (and by the last bit of
+ * the rotation's terms), and codes of such keys may be neighbours: the last multiplication, addition and
+ * rounding may be one instruction in one call and several in the other. */
 pv_status pv_kv8_norm_rope_append_planned(pv_plan *plan, const void *q_in, void *q_out,
                                           const void *k_new, const void *v_new,
                                           const void *q_weight, const void *k_weight, float eps,
@@ -442,9 +449,9 @@ pv_status pv_kv8_read_planned(pv_plan *plan, const pv_kv8_pool *pool, const int3
 /*
  * Multi-token paged attention over 8-bit pools: pv_multi_token_paged_attn_planned with K, V = code *
  * 2^e.  Codes are widened to the 16-bit type on the way to the matrix cores, which is exact; everything
- * behind that is as there (scores, softmax and sums in fp32, probabilities and results rounded to
- * 16 bits).  Arguments, workspace and launches as there.  A NaN code reaches the rows that see its
- * position and no others.
+ * behind that is as there (scores, softmax and sums in fp32, results rounded to 16 bits; probabilities
+ * rounded to 16 bits, without the second term that some plans for 16-bit pools have).  Arguments,
+ * workspace and launches as there.  A NaN code reaches the rows that see its position and no others.
  */
 pv_status pv_kv8_multi_token_paged_attn_planned(pv_plan *plan, const void *q,
                                                 const pv_kv8_pool *pool,
