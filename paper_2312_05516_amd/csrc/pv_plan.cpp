@@ -86,7 +86,7 @@ static int64_t item_cost(const WorkItem &w) { return w.kv_end - w.kv_begin; }
 // into parts of about `chunk` keys, evened out and rounded up to whole blocks.
 struct Cut {
     int64_t chunk, longest_whole, min_keys;
-    int32_t block = kKvBlock;  // keys of the kernel's inner step
+    int32_t block_log2 = kKvBlockLog2;  // of the keys of the kernel's inner step
     int32_t parts(int64_t len) const
     {
         return len <= longest_whole || len < 2 * min_keys ? 1 : ((int32_t)len - 1) / part_len(len) + 1;
@@ -95,7 +95,7 @@ struct Cut {
     int32_t part_len(int64_t len) const
     {
         const uint32_t keys = (uint32_t)len, n = (keys - 1) / (uint32_t)chunk + 1;
-        return (int32_t)(((keys - 1) / n + (uint32_t)block) / (uint32_t)block * (uint32_t)block);
+        return (int32_t)((((keys - 1) / n >> block_log2) + 1) << block_log2);
     }
 };
 
@@ -121,7 +121,7 @@ struct CutRule {
     int32_t key_ns;      // what a key less in the longest item saves while the GPU is not full
     int32_t always_cut;  // up to this many parts that is not weighed against the merge
     bool level_lists;    // lists of nearly equal items go by how full their last round of CUs is
-    int32_t block;       // parts are whole numbers of so many keys
+    int32_t block_log2;  // parts are whole numbers of so many keys
     bool whole_counts;   // a cut saves no more than the longest item that it leaves whole lets it
 };
 
@@ -225,7 +225,7 @@ static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &
     const Cut even = target_cut(total_keys, items.size(), tune.split_target, tune);
     Cut cut = given ? *given : even;
     if (rule) {
-        cut.block = rule->block;
+        cut.block_log2 = rule->block_log2;
         auto blocks = [](int64_t keys) { return (keys + kKvBlock - 1) / kKvBlock * kKvBlock; };
         const int64_t n = (int64_t)items.size();
         if (rule->level_lists && n > rule->slots && n < tune.split_target &&
@@ -238,7 +238,7 @@ static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &
             cut.longest_whole = cut.chunk + cut.chunk / 4;
         } else if (rule->always_stretch || n <= rule->slots) {
             auto at_once = [&](int64_t chunk) {
-                const Cut c = {chunk, chunk, cut.min_keys, cut.block};
+                const Cut c = {chunk, chunk, cut.min_keys, cut.block_log2};
                 int64_t parts = 0;
                 for (const Shape &s : shapes) parts += c.parts(s.len);
                 return parts * heads <= rule->slots;
@@ -309,7 +309,7 @@ static bool split_items(std::vector<WorkItem> &items, std::vector<CombineItem> &
             continue;
         }
         int64_t part_len = (len + parts - 1) / parts;
-        part_len = (part_len + cut.block - 1) / cut.block * cut.block;
+        part_len = (((part_len - 1) >> cut.block_log2) + 1) << cut.block_log2;
         parts = (len + part_len - 1) / part_len;
         if (parts <= 1) {
             result.push_back(w);
@@ -605,11 +605,11 @@ pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_
     }
 
     // append: runs of new tokens that share an 8-slot group of a page (a page, for 8-bit pools)
-    const int64_t run = kv8 ? 16 : 8;
+    const int run_log2 = kv8 ? 4 : 3;  // (a division each is 7 % of the time of plans for prompts)
     for (int32_t r = 0; r < num_reqs; ++r) {
         const int64_t c = ctx_lens[r], end = (int64_t)ctx_lens[r] + q_lens[r];
         for (int64_t t = c; t < end;) {
-            const int64_t group_end = (t / run + 1) * run;
+            const int64_t group_end = ((t >> run_log2) + 1) << run_log2;
             const int64_t stop = std::min(end, group_end);
             AppendGroup g;
             g.req = r;
@@ -783,9 +783,9 @@ pv_status build_plan(const pv_pool_desc *pool, int32_t num_q_heads, const int32_
                                           : (int64_t)plan->narrow.size() > kNarrowSlots ? 12 : 9;
     const CutRule narrow_rule = {
         kNarrowSlots, wide_rows ? kNarrowSlots * 5 / 4 : 0, kNarrowSlots, 25, false, narrow_ns, 0, true,
-        kv8 ? 2 * kKvBlock : kKvBlock, kv8};
+        kv8 ? kKvBlockLog2 + 1 : kKvBlockLog2, kv8};
     const CutRule wide_rule = {kWideSlots, kFewWideItems, kFewWideItems, 100, true,
-                               wide_rows ? 31 : 16, wide_rows ? kCUs : 0, false, kKvBlock, true};
+                               wide_rows ? 31 : 16, wide_rows ? kCUs : 0, false, kKvBlockLog2, true};
     plan->narrow_two_terms =
         split_items(plan->narrow, plan->combine, slots, tune, &narrow_rule, pool->head_dim);
     plan->wide_renews =

@@ -193,7 +193,8 @@ constexpr int kWideSlots = 768;
 constexpr int kItemSetUp = 96;  // keys that take an item as long as its set-up and its result
 constexpr int kSplitTarget = 1024;
 constexpr int kFewWideItems = 512;  // shorter lists of the 128-row kernel are cut to fill the GPU
-constexpr int kKvBlock = 32;     // keys per inner step (two pages)
+constexpr int kKvBlockLog2 = 5;
+constexpr int kKvBlock = 1 << kKvBlockLog2;  // keys per inner step (two pages)
 constexpr float kLazyLog2 = 8.f;  // matrix-core kernels: the reference maximum of a row may lag the
                                   // true one by this many powers of 2
 constexpr int kTileMaxPages = 8192;  // page ids an item of the 256-row kernel may span (it keeps
