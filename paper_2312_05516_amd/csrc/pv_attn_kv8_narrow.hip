@@ -170,6 +170,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_narrow_kernel(
 #pragma unroll
             for (int blk = 0; blk < NB; ++blk) o[blk] *= alpha;
         }
+        // The probabilities are rounded to 16 bits for the product with V, their sum is not: results are
+        // 1.8e-3 from 64 bits in bf16 (relative 2-norm; the rounding of the result alone 1.66e-3), and 6 %
+        // of the time of short lists would buy a second term that takes that back.
         u32x4 p[2];
 #pragma unroll
         for (int jj = 0; jj < 8; ++jj) p[jj / 4][jj % 4] = T::pack2(x[2 * jj], x[2 * jj + 1]);

@@ -44,9 +44,11 @@ namespace pv {
 // test for it in the loop they take 1 % longer.
 // KV8: the pools hold 8-bit codes (pv_kv8.h).  Their blocks go through registers: every thread reads 16
 // codes of K and 16 of V, a block ahead, and stores them widened to 16 bits in LDS, in the layout that
-// the copies of 16-bit pages have there, so that a code is converted once for all rows of the item.  Bound
-// as over 16-bit pools: 48 requests, 64/8 heads, 3 of 5 generation steps, 117 GFLOP in 142-154 us; neither 20
-// vector instructions nor 20 KiB of LDS traffic a block fewer changed that.
+// the copies of 16-bit pages have there, so that a code is converted once for all rows of the item.  Bound:
+// vector and matrix work one behind the other (a wavefront widens a block between two blocks' products).  48
+// requests, 64/8 heads, 3 of 5 generation steps, 117 GFLOP in 142-154 us: matrix pipe busy in 38 % of the SIMD
+// cycles, vector ALU in 50 %, at 2.05 GHz; head size 64, 32/8 heads, 66 GFLOP in 101 us: 30 and 56 %.  Neither 20
+// vector instructions nor 20 KiB of LDS traffic a block fewer changed that.  Two of the three stages are used.
 template <typename T, int D, bool RENEW, bool STREAMS, bool KV8>
 __global__ __launch_bounds__(256, 3) void attn_wide_kernel(
     const WorkItem *__restrict__ items, const uint16_t *__restrict__ q,

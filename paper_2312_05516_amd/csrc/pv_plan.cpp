@@ -128,7 +128,9 @@ struct CutRule {
 // How to cut the 256-row kernel's list over 8-bit pools.  One workgroup runs on a CU, so the time of a
 // list is that of the CU with the most keys, when the longest part goes first to the CU that is free
 // first (25 ns a key and 2.5 us an item), and a cut costs the merge besides.  Of a few cuts the best by
-// that count: 512 tiles over 19-25 K keys, two to a CU, take 1217 us whole and 1297 in 1024 parts.
+// that count: 512 tiles over 19-25 K keys, two to a CU, take 1217 us whole and 1297 in 1024 parts, the batch that
+// the constants come from.  The count takes host time: a plan for 16 requests of 512 tokens over 20 K keys, 64/8 heads,
+// 225 us (45 without it), over 19-25 K keys 640 (46); lists of more than eight tiles a CU are not counted.
 static Cut tile_cut(const std::vector<WorkItem> &tiles, int32_t head_dim, const Tuning &tune)
 {
     int64_t total = 0;

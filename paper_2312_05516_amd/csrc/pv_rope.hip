@@ -21,7 +21,7 @@ namespace pv {
 
 // NORM: rows whose kind has a weight are first scaled to y = x * w / sqrt(mean(x^2) + eps), in fp32
 // and without a rounding of their own; the lanes that hold a row are neighbours.  Bound: HBM, as without.
-// 6 prompts, 4.8 K tokens, 40/40 heads: 296 MB in 62 us = 4.8 TB/s (between calls).
+// 6 prompts, 4.8 K tokens, 40/40 heads: 296 MB in 62.3 us = 4.8 TB/s (between calls).
 //
 // kVApart: V in workgroups of its own, in front of the others.  Behind K's norms and rotation its loads come
 // late: the same 6 prompts 65.2 us otherwise, 63.0 so (half pairs 62.4 and 61.6, 64/8 heads the same; head
